@@ -358,6 +358,88 @@ int scd_objective_static(const scd_matrix_t *A, const float *y_dev, double lambd
                          const float *model_dev, const float *shared_dev, void *stream, double *primal,
                          double *dual);
 
+/* ---- Learned features -------------------------------------------------------------------------
+ * Operators for models whose coordinates are not one-hot columns but rows of a learned table: ids are
+ * looked up (scd_embed), the vectors normalised (scd_layer_norm), a read-out is fitted on them by the
+ * solver above, and the table is trained by the read-out's gradient, which goes back through both
+ * (scd_layer_norm_grad, scd_embed_grad) and is clipped by its global norm (scd_clip_grads).
+ *
+ * Conventions of these calls:
+ *   - They take no handle, keep nothing between calls, enqueue on `stream` only and never synchronise;
+ *     they allocate nothing: scratch is the caller's (workspace calls), so they can be captured in graphs.
+ *     The workspace may be reused by the next call on the same stream.
+ *   - Elements are SCD_F32, SCD_BF16 or SCD_F16 and aligned to their size; sums, means and statistics
+ *     are held in 32 bits (the clipping norm in 64) and every output is rounded once.
+ *   - A matrix of n rows and dim columns has unit column stride; row strides are in elements, at least
+ *     dim for outputs, and any value (0: one row for all) for inputs.  Outputs overlap no input unless
+ *     said otherwise.  dim is in [1, 2^20], row counts are below 2^31; a count of rows may be 0.
+ *   - Results are bit-identical from call to call: no sum depends on the order in which waves run.
+ * Errors: SCD_ERR_INVALID (null pointer, size, stride, unaligned workspace), SCD_ERR_UNSUPPORTED (a
+ * type, or a pair of types, that the call does not take), SCD_ERR_HIP. */
+typedef enum { SCD_F32 = 0, SCD_BF16 = 1, SCD_F16 = 2, SCD_I32 = 3, SCD_I64 = 4 } scd_type_t;
+
+/* out[t, :] = scale * table[tokens[t], :], t < n.  A negative token is a padded place and gives zeros; a
+ * token of at least `rows` names no row and gives NaN.
+ *   tokens_dev: SCD_I32 or SCD_I64 [n];  table_dev: [rows, dim];  out_dev: [n, dim], of any element type. */
+int scd_embed(const void *tokens_dev, int32_t token_type, int64_t n, const void *table_dev, int32_t table_type,
+              int64_t table_stride, int64_t rows, int64_t dim, float scale, void *out_dev, int32_t out_type,
+              int64_t out_stride, void *stream);
+
+/* The gradient of scd_embed with respect to its table: out[v, :] = scale * sum of grad[t, :] over the t with
+ * tokens[t] = v, in ascending order of t up to the split of long runs; rows without a token get zeros, tokens
+ * outside [0, rows) add to nothing (their gradients are not read).  accumulate = 1 adds this to what out
+ * holds, and leaves rows without a token as they are.
+ *   grad_dev: [n, dim];  out_dev: [rows, dim], of any element type.
+ * The tokens are sorted first (a stable radix sort), so that each row is summed by its owner and written
+ * once, without atomics.  scd_embed_grad_workspace gives the bytes of scratch that a call needs (16-byte
+ * aligned, device). */
+int scd_embed_grad_workspace(int64_t n, int64_t rows, int64_t dim, int64_t *bytes);
+int scd_embed_grad(const void *tokens_dev, int32_t token_type, int64_t n, const void *grad_dev, int32_t grad_type,
+                   int64_t grad_stride, int64_t rows, int64_t dim, float scale, int32_t accumulate, void *out_dev,
+                   int32_t out_type, int64_t out_stride, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* y[r, :] = (x[r, :] - mean[r]) * rstd[r] * weight + bias, mean and rstd = 1/sqrt(var + eps) over the row,
+ * var = mean of (x - mean)^2.
+ *   x_dev, y_dev: [rows, dim] of `type` (y may be x);  weight_dev, bias_dev: [dim] of param_type (`type` or
+ *   SCD_F32), either may be NULL (1, 0);  mean_dev, rstd_dev: float32[rows], NULL to leave them out.
+ *   eps >= 0. */
+int scd_layer_norm(const void *x_dev, int32_t type, int64_t x_stride, int64_t rows, int64_t dim, const void *weight_dev,
+                   const void *bias_dev, int32_t param_type, float eps, void *y_dev, int64_t y_stride, float *mean_dev,
+                   float *rstd_dev, void *stream);
+
+/* The gradients of scd_layer_norm.  With h = (x - mean) * rstd and g = grad * weight, all over the row:
+ *   dx = rstd * (g - mean(g) - h * mean(g * h));   dweight = sum over rows of grad * h;   dbias = sum of grad.
+ *   grad_dev, x_dev, dx_dev: [rows, dim] of `type` (dx may be grad or x);  mean_dev, rstd_dev: float32[rows] as
+ *   scd_layer_norm wrote them;  weight_dev: [dim] of param_type or NULL (1);  dweight_dev, dbias_dev: [dim]
+ *   of param_type, both or neither NULL.
+ * scd_layer_norm_grad_workspace: bytes of scratch (16-byte aligned, device), 0 where dweight is NULL. */
+int scd_layer_norm_grad_workspace(int64_t rows, int64_t dim, int64_t *bytes);
+int scd_layer_norm_grad(const void *grad_dev, int64_t grad_stride, const void *x_dev, int64_t x_stride, int32_t type,
+                        const float *mean_dev, const float *rstd_dev, int64_t rows, int64_t dim, const void *weight_dev,
+                        int32_t param_type, void *dx_dev, int64_t dx_stride, void *dweight_dev, void *dbias_dev,
+                        void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* One tensor of scd_clip_grads: n elements at src, of src_type, written to dst as dst_type (src_type or
+ * SCD_F32).  dst may be src (same type); otherwise spans overlap no other. */
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t n;
+    int32_t src_type;
+    int32_t dst_type;
+} scd_span_t;
+
+/* Clips `count` >= 0 tensors together by their norm: norm = sqrt(sum of the squares of all elements), factor =
+ * max_norm / norm if norm > max_norm, else 1; dst = factor * src for every span.  Where dst is src, a factor of
+ * 1 writes nothing; a span whose dst is NULL only counts towards the norm.  Squares are summed in 64 bits, so no
+ * finite input overflows.  A NaN makes norm and factor NaN, an infinity makes norm infinite and factor 0, so
+ * that both show in what is written (with max_norm = infinity the factor of an infinite norm is 1).
+ *   spans: host array (read before the call returns);  max_norm >= 0 (infinity: the norm alone is of interest);
+ *   norm_dev: float32[1], device;  workspace_dev: scd_clip_grads_workspace bytes (16-byte aligned, device). */
+int scd_clip_grads_workspace(int64_t *bytes);
+int scd_clip_grads(const scd_span_t *spans, int64_t count, float max_norm, float *norm_dev, void *workspace_dev,
+                   int64_t workspace_bytes, void *stream);
+
 /* Message describing the last error on the calling thread ("" if none). */
 const char *scd_last_error(void);
 

@@ -5,4 +5,4 @@ models (arXiv 1702.07005): HIP kernels for gfx950 behind the C ABI declared in
 Importing the package loads nothing; the HIP library is loaded on first use of
 ``paper_1702_07005_amd.scd``.
 """
-__all__ = ["scd", "synth"]
+__all__ = ["scd", "features", "synth"]

@@ -1,0 +1,490 @@
+// scd_norm.hip -- layer norm over the columns of a matrix, and its gradients (gfx950).
+//
+// Forward: m = mean x, v = mean (x - m)^2, r = 1/sqrt(v + eps), y = (x - m) r w + b.
+// Backward, h = (x - m) r, g = dy w:  dx = r (g - mean g - h mean(g h)), dw = sum_rows dy h, db = sum_rows dy.
+//
+// Both are bound by memory: the forward pass reads and writes the matrix once, the backward pass reads two and
+// writes one.  A row stays in the registers of a group of lanes between its statistics and its result, so that it is
+// read once and the variance is that of the centred values.  Groups walk the rows with a fixed stride; the
+// backward pass keeps its share of dw and db in registers on the way, each workgroup writes its sums to the
+// workspace in 32 bits, and a second kernel adds the workgroups' in a fixed order.
+#include <algorithm>
+
+#include "scd_device.h"
+#include "scd_feat.h"
+
+namespace scd {
+namespace feat {
+namespace {
+
+// The columns of a lane's NV vectors: vector j of lane l is the (l + j LPR)-th of the row.
+template <int VEC, int NV, int LPR>
+struct Columns {
+    int32_t at[NV];
+    int32_t skip[NV];  // leading columns that another lane counts; VEC where the row has no such vector
+    __device__ __forceinline__ Columns(int32_t lane, int32_t dim) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int32_t k = lane + j * LPR;
+            at[j] = vec_column<VEC>(k, dim, skip[j]);
+            skip[j] = min(skip[j], VEC);
+        }
+    }
+};
+
+// The sums of K values over each group of LPR lanes.  Groups wider than a wave go through LDS; `turn` alternates
+// from call to call, so that one barrier a call is enough.
+template <int LPR, int THREADS, int K>
+__device__ __forceinline__ void group_sums(float (&s)[K], float* lds, int turn) {
+    if constexpr (LPR <= 64) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[k] = group_sum<LPR>(s[k]);
+    } else {
+        constexpr int kWaves = LPR / 64;
+        float* const mine = lds + turn * (THREADS / 64) * K + (threadIdx.x / LPR) * kWaves * K;
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[k] = group_sum<64>(s[k]);
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) mine[threadIdx.x % LPR / 64 * K + k] = s[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            s[k] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) s[k] += mine[w * K + k];
+        }
+    }
+}
+
+template <int LPR, int THREADS>
+constexpr int lds_words(int k) {
+    return LPR <= 64 ? 1 : 2 * (THREADS / 64) * k;
+}
+
+template <typename T, typename P>
+struct NormArgs {
+    const T* x;
+    int64_t xstride;
+    int32_t rows;
+    int32_t dim;
+    const P* weight;
+    const P* bias;
+    float eps;
+    T* y;
+    int64_t ystride;
+    float* mean;
+    float* rstd;
+};
+
+template <int VEC, int NV, int LPR, int THREADS, typename T, typename P>
+__global__ void __launch_bounds__(THREADS) k_norm(NormArgs<T, P> a) {
+    __shared__ float lds[lds_words<LPR, THREADS>(2)];
+    constexpr int kGroups = THREADS / LPR;
+    const int32_t lane = threadIdx.x % LPR;
+    const int64_t g = (int64_t)blockIdx.x * kGroups + threadIdx.x / LPR, step = (int64_t)gridDim.x * kGroups;
+    const Columns<VEC, NV, LPR> col(lane, a.dim);
+    const float inv = 1.0f / (float)a.dim;
+    Raw<VEC, T> next[NV];
+    Raw<VEC, P> w[NV], b[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) next[j] = load_raw<VEC>(a.x + min(g, (int64_t)a.rows - 1) * a.xstride + col.at[j]);
+    if (a.weight)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) w[j] = load_raw<VEC>(a.weight + col.at[j]);
+    else
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[j].t[i] = (P)1.0f;
+    if (a.bias)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) b[j] = load_raw<VEC>(a.bias + col.at[j]);
+    else
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) b[j].t[i] = (P)0.0f;
+    // Every group of a workgroup takes as many turns, those past the last row on that row and without a result.
+    for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < a.rows; r0 += step) {
+        const int64_t r = r0 + threadIdx.x / LPR;
+        float x[NV][VEC];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) widen(next[j], x[j]);
+        if (r0 + step < a.rows)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) next[j] = load_raw<VEC>(a.x + min(r + step, (int64_t)a.rows - 1) * a.xstride + col.at[j]);
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s[0] += i >= col.skip[j] ? x[j][i] : 0.0f;
+        group_sums<LPR, THREADS, 1>(s, lds, 0);
+        const float mean = s[0] * inv;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                x[j][i] -= mean;
+                s[0] += i >= col.skip[j] ? x[j][i] * x[j][i] : 0.0f;
+            }
+        group_sums<LPR, THREADS, 1>(s, lds, 1);
+        const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
+        if (r < a.rows) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float wj[VEC], bj[VEC], y[VEC];
+                widen(w[j], wj);
+                widen(b[j], bj);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) y[i] = x[j][i] * rstd * wj[i] + bj[i];
+                if (col.skip[j] < VEC) store_vec(a.y + r * a.ystride + col.at[j], y);
+            }
+            if (lane == 0) {
+                if (a.mean) a.mean[r] = mean;
+                if (a.rstd) a.rstd[r] = rstd;
+            }
+        }
+    }
+}
+
+// Rows too wide for the registers: a workgroup reads its row three times (from the caches after the first).
+constexpr int kWideThreads = 1024;
+
+template <typename T, typename P>
+__global__ void __launch_bounds__(kWideThreads) k_norm_wide(NormArgs<T, P> a) {
+    __shared__ float lds[lds_words<kWideThreads, kWideThreads>(1)];
+    const float inv = 1.0f / (float)a.dim;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T* const x = a.x + r * a.xstride;
+        T* const y = a.y + r * a.ystride;
+        float s[1] = {0.0f};
+        for (int32_t c = threadIdx.x; c < a.dim; c += kWideThreads) s[0] += (float)x[c];
+        group_sums<kWideThreads, kWideThreads, 1>(s, lds, 0);
+        const float mean = s[0] * inv;
+        s[0] = 0.0f;
+        for (int32_t c = threadIdx.x; c < a.dim; c += kWideThreads) {
+            const float d = (float)x[c] - mean;
+            s[0] += d * d;
+        }
+        group_sums<kWideThreads, kWideThreads, 1>(s, lds, 1);
+        const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
+        for (int32_t c = threadIdx.x; c < a.dim; c += kWideThreads) {
+            const float w = a.weight ? (float)a.weight[c] : 1.0f, b = a.bias ? (float)a.bias[c] : 0.0f;
+            y[c] = (T)(((float)x[c] - mean) * rstd * w + b);
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[r] = mean;
+            if (a.rstd) a.rstd[r] = rstd;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------- backward
+
+template <typename T, typename P>
+struct NormGradArgs {
+    const T* dy;
+    int64_t gstride;
+    const T* x;
+    int64_t xstride;
+    const float* mean;
+    const float* rstd;
+    int32_t rows;
+    int32_t dim;
+    const P* weight;
+    T* dx;
+    int64_t dstride;
+    float* sums;  // [workgroups][2][dim] of dw and db, or null
+};
+
+template <int VEC, int NV, int LPR, int THREADS, typename T, typename P>
+__global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
+    constexpr int kGroups = THREADS / LPR;
+    constexpr int kElems = LPR * NV * VEC;
+    __shared__ float lds[lds_words<LPR, THREADS>(2)];
+    __shared__ float part[kGroups > 1 ? kGroups * kElems : 1];
+    // The next row is loaded ahead, but not where a thread's share of the row leaves no registers for it.
+    constexpr bool kAhead = THREADS < 1024;
+    const int32_t lane = threadIdx.x % LPR;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const Columns<VEC, NV, LPR> col(lane, a.dim);
+    const float inv = 1.0f / (float)a.dim;
+    Raw<VEC, T> ndy[NV], nx[NV];
+    Raw<VEC, P> w[NV];
+    float nmean, nrstd, dw[NV][VEC] = {}, db[NV][VEC] = {};
+    const auto fetch = [&](int64_t row) {
+        row = min(row, (int64_t)a.rows - 1);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) ndy[j] = load_raw<VEC>(a.dy + row * a.gstride + col.at[j]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) nx[j] = load_raw<VEC>(a.x + row * a.xstride + col.at[j]);
+        nmean = a.mean[row];
+        nrstd = a.rstd[row];
+    };
+    if (kAhead) fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
+    if (a.weight)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) w[j] = load_raw<VEC>(a.weight + col.at[j]);
+    else
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[j].t[i] = (P)1.0f;
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
+        const int64_t r = r0 + threadIdx.x / LPR;
+        if (!kAhead) fetch(r);
+        float dy[NV][VEC], h[NV][VEC], s[2] = {0.0f, 0.0f};
+        const float mean = nmean, rstd = nrstd, here = r < a.rows ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            widen(ndy[j], dy[j]);
+            widen(nx[j], h[j]);
+        }
+        if (kAhead && r0 + step < a.rows) fetch(r + step);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float wj[VEC];
+            widen(w[j], wj);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                h[j][i] = (h[j][i] - mean) * rstd;
+                if (here != 0.0f) {
+                    dw[j][i] += dy[j][i] * h[j][i];
+                    db[j][i] += dy[j][i];
+                }
+                dy[j][i] *= wj[i];
+                s[0] += i >= col.skip[j] ? dy[j][i] : 0.0f;
+                s[1] += i >= col.skip[j] ? dy[j][i] * h[j][i] : 0.0f;
+            }
+        }
+        group_sums<LPR, THREADS, 2>(s, lds, turn);
+        const float c1 = s[0] * inv, c2 = s[1] * inv;
+        if (r < a.rows) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) dy[j][i] = rstd * (dy[j][i] - c1 - h[j][i] * c2);
+                if (col.skip[j] < VEC) store_vec(a.dx + r * a.dstride + col.at[j], dy[j]);
+            }
+        }
+    }
+    if (!a.sums) return;
+    float* const out = a.sums + (int64_t)blockIdx.x * 2 * a.dim;
+    for (int which = 0; which < 2; ++which) {
+        if constexpr (kGroups > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    part[(threadIdx.x / LPR) * kElems + (lane + j * LPR) * VEC + i] = which ? db[j][i] : dw[j][i];
+            __syncthreads();
+            for (int e = threadIdx.x; e < kElems; e += THREADS) {
+                int32_t again;
+                const int32_t c = vec_column<VEC>(e / VEC, a.dim, again) + e % VEC;
+                if (e % VEC < again) continue;
+                float s = 0.0f;
+#pragma unroll
+                for (int k = 0; k < kGroups; ++k) s += part[k * kElems + e];
+                out[which * a.dim + c] = s;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (col.skip[j] < VEC) store_vec(out + which * a.dim + col.at[j], which ? db[j] : dw[j]);
+        }
+    }
+}
+
+template <typename T, typename P>
+__global__ void __launch_bounds__(kWideThreads) k_norm_grad_wide(NormGradArgs<T, P> a) {
+    __shared__ float lds[lds_words<kWideThreads, kWideThreads>(2)];
+    const float inv = 1.0f / (float)a.dim;
+    float* const dw = a.sums ? a.sums + (int64_t)blockIdx.x * 2 * a.dim : nullptr;
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+        const T* const dy = a.dy + r * a.gstride;
+        const T* const x = a.x + r * a.xstride;
+        T* const dx = a.dx + r * a.dstride;
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float s[2] = {0.0f, 0.0f};
+        for (int32_t c = threadIdx.x; c < a.dim; c += kWideThreads) {
+            const float d = (float)dy[c], h = ((float)x[c] - mean) * rstd, g = d * (a.weight ? (float)a.weight[c] : 1.0f);
+            s[0] += g;
+            s[1] += g * h;
+            if (dw) {  // each thread its own columns
+                const bool first = r == blockIdx.x;
+                dw[c] = (first ? 0.0f : dw[c]) + d * h;
+                dw[a.dim + c] = (first ? 0.0f : dw[a.dim + c]) + d;
+            }
+        }
+        group_sums<kWideThreads, kWideThreads, 2>(s, lds, turn);
+        const float c1 = s[0] * inv, c2 = s[1] * inv;
+        for (int32_t c = threadIdx.x; c < a.dim; c += kWideThreads) {
+            const float h = ((float)x[c] - mean) * rstd, g = (float)dy[c] * (a.weight ? (float)a.weight[c] : 1.0f);
+            dx[c] = (T)(rstd * (g - c1 - h * c2));
+        }
+    }
+}
+
+// dw and db: the workgroups' sums, 64 columns a workgroup, in kSlices interleaved parts that are added in order.
+constexpr int kSlices = 16;
+
+template <typename P>
+__global__ void __launch_bounds__(64 * kSlices) k_norm_params(const float* __restrict__ sums, int32_t parts, int32_t dim,
+                                                              P* __restrict__ dw, P* __restrict__ db) {
+    __shared__ float lds[kSlices][64];
+    const int64_t c = (int64_t)blockIdx.x * 64 + threadIdx.x % 64, width = 2 * (int64_t)dim;
+    const int32_t slice = threadIdx.x / 64;
+    float s = 0.0f;
+    if (c < width)
+#pragma unroll 8
+        for (int32_t p = slice; p < parts; p += kSlices) s += sums[p * width + c];
+    lds[slice][threadIdx.x % 64] = s;
+    __syncthreads();
+    if (slice == 0 && c < width) {
+#pragma unroll
+        for (int k = 1; k < kSlices; ++k) s += lds[k][threadIdx.x];
+        if (c < dim)
+            dw[c] = (P)s;
+        else
+            db[c - dim] = (P)s;
+    }
+}
+
+// ---------------------------------------------------------------------------------------- host
+
+// Calls f(Int<VEC>, Int<NV>, Int<LPR>) with the smallest group that holds a row of `dim` elements of T, or returns
+// false where none does.
+template <typename T, typename F>
+bool with_group(int64_t dim, F&& f) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t vecs = ceil_div(dim, V);
+    if (dim < V)
+        f(Int<1>{}, Int<1>{}, Int<8>{});
+    else if (vecs <= 4)
+        f(Int<V>{}, Int<1>{}, Int<4>{});
+    else if (vecs <= 8)
+        f(Int<V>{}, Int<1>{}, Int<8>{});
+    else if (vecs <= 16)
+        f(Int<V>{}, Int<1>{}, Int<16>{});
+    else if (vecs <= 32)
+        f(Int<V>{}, Int<1>{}, Int<32>{});
+    else if (vecs <= 64)
+        f(Int<V>{}, Int<1>{}, Int<64>{});
+    else if (vecs <= 128)
+        f(Int<V>{}, Int<2>{}, Int<64>{});
+    else if (vecs <= 256)
+        f(Int<V>{}, Int<1>{}, Int<256>{});
+    else if (vecs <= 512)
+        f(Int<V>{}, Int<2>{}, Int<256>{});
+    else if (vecs <= 1024)
+        f(Int<V>{}, Int<2>{}, Int<512>{});
+    else if (vecs <= 2048)
+        f(Int<V>{}, Int<2>{}, Int<1024>{});
+    else
+        return false;
+    return true;
+}
+
+constexpr int kNormThreads = 256;   // a workgroup, where a row's group is not wider
+constexpr int kBlocks = 2048;       // workgroups at most: eight to each CU
+constexpr int kGradBlocks = 512;    // the backward pass's, whose sums of dw and db go through memory
+
+template <typename F>
+void with_types(int32_t type, int32_t param, F&& f) {
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        if constexpr (sizeof(T) == 4)
+            f(t, t);
+        else
+            param == SCD_F32 ? f(t, float{}) : f(t, t);
+    });
+}
+
+int check_norm(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {
+    if (!type_bytes(type) || (param_type != type && param_type != SCD_F32))
+        return fail(SCD_ERR_UNSUPPORTED, "layer norm takes float32, bfloat16 or float16 with parameters of that type or float32");
+    if (rows < 0 || rows > kMaxRows || dim < 1 || dim > kMaxDim)
+        return fail(SCD_ERR_INVALID, "bad sizes rows=%lld dim=%lld", (long long)rows, (long long)dim);
+    return SCD_OK;
+}
+
+int64_t grad_blocks(int64_t rows) { return std::min<int64_t>(rows, kGradBlocks); }
+
+}  // namespace
+}  // namespace feat
+}  // namespace scd
+
+using namespace scd::feat;
+
+extern "C" int scd_layer_norm(const void* x, int32_t type, int64_t x_stride, int64_t rows, int64_t dim, const void* weight,
+                              const void* bias, int32_t param_type, float eps, void* y, int64_t y_stride, float* mean,
+                              float* rstd, void* stream) {
+    if (int r = check_norm(type, param_type, rows, dim)) return r;
+    if (!(eps >= 0.0f)) return fail(SCD_ERR_INVALID, "eps must be >= 0");
+    if (x_stride < 0 || (y_stride < dim && rows > 1)) return fail(SCD_ERR_INVALID, "bad row stride");
+    if (x == y && rows > 1 && x_stride != y_stride) return fail(SCD_ERR_INVALID, "in place the strides must be the same");
+    if (rows == 0) return SCD_OK;
+    if (!x || !y) return fail(SCD_ERR_INVALID, "null device pointer");
+    hipStream_t s = (hipStream_t)stream;
+    with_types(type, param_type, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        const NormArgs<T, P> a{(const T*)x, x_stride, (int32_t)rows, (int32_t)dim, (const P*)weight, (const P*)bias, eps, (T*)y, y_stride, mean, rstd};
+        const bool fits = with_group<T>(dim, [&](auto vec, auto nv, auto lpr) {
+            constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
+            constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
+            const int64_t blocks = std::min<int64_t>(kBlocks, ceil_div(rows, THREADS / LPR));
+            k_norm<VEC, NV, LPR, THREADS><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+        });
+        if (!fits) k_norm_wide<<<(uint32_t)std::min<int64_t>(kBlocks, rows), kWideThreads, 0, s>>>(a);
+    });
+    return launched("scd_layer_norm");
+}
+
+extern "C" int scd_layer_norm_grad_workspace(int64_t rows, int64_t dim, int64_t* bytes) {
+    if (!bytes) return fail(SCD_ERR_INVALID, "bytes is null");
+    *bytes = 0;
+    if (int r = check_norm(SCD_F32, SCD_F32, rows, dim)) return r;
+    *bytes = grad_blocks(rows) * 2 * dim * 4;
+    return SCD_OK;
+}
+
+extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int32_t type,
+                                   const float* mean, const float* rstd, int64_t rows, int64_t dim, const void* weight,
+                                   int32_t param_type, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                                   void* workspace, int64_t workspace_bytes, void* stream) {
+    if (int r = check_norm(type, param_type, rows, dim)) return r;
+    if (grad_stride < 0 || x_stride < 0 || (dx_stride < dim && rows > 1)) return fail(SCD_ERR_INVALID, "bad row stride");
+    if (rows > 1 && ((dx == grad && dx_stride != grad_stride) || (dx == x && dx_stride != x_stride)))
+        return fail(SCD_ERR_INVALID, "in place the strides must be the same");
+    if (!dweight != !dbias) return fail(SCD_ERR_INVALID, "dweight and dbias go together");
+    if (rows > 0 && (!grad || !x || !mean || !rstd || !dx)) return fail(SCD_ERR_INVALID, "null device pointer");
+    const int64_t need = dweight ? grad_blocks(rows) * 2 * dim * 4 : 0;
+    if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need))
+        return fail(SCD_ERR_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)need);
+    hipStream_t s = (hipStream_t)stream;
+    with_types(type, param_type, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        float* const sums = dweight ? (float*)workspace : nullptr;
+        const NormGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)x, x_stride, mean, rstd, (int32_t)rows, (int32_t)dim, (const P*)weight, (T*)dx, dx_stride, sums};
+        int64_t blocks = grad_blocks(rows);
+        if (rows > 0) {
+            const bool fits = with_group<T>(dim, [&](auto vec, auto nv, auto lpr) {
+                constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
+                constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
+                blocks = std::min<int64_t>(blocks, ceil_div(rows, THREADS / LPR));
+                k_norm_grad<VEC, NV, LPR, THREADS><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+            });
+            if (!fits) k_norm_grad_wide<<<(uint32_t)blocks, kWideThreads, 0, s>>>(a);
+        }
+        if (dweight)
+            k_norm_params<<<(uint32_t)ceil_div(2 * dim, 64), 64 * kSlices, 0, s>>>((const float*)workspace, (int32_t)blocks, (int32_t)dim, (P*)dweight, (P*)dbias);
+    });
+    return launched("scd_layer_norm_grad");
+}
