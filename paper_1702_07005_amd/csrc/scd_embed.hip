@@ -72,6 +72,10 @@ __global__ void __launch_bounds__(kThreads) k_embed(const TI* __restrict__ tok, 
 
 constexpr int kBatch = 8;
 
+struct __align__(8) Pair {
+    uint32_t key, pos;
+};
+
 template <typename TI>
 struct Tokens {
     const TI* tok;
@@ -81,13 +85,12 @@ struct Tokens {
         const int64_t t = i < n ? (int64_t)tok[i] : -1;
         return t >= 0 && t < (int64_t)rows ? (uint32_t)t : rows;
     }
-    __device__ uint32_t pos(int64_t i) const { return i < n ? (uint32_t)i : 0; }
+    __device__ Pair pair(int64_t i) const { return Pair{key(i), i < n ? (uint32_t)i : 0}; }
 };
 struct Pairs {
-    const uint32_t* k;
-    const uint32_t* p;
-    __device__ uint32_t key(int64_t i) const { return k[i]; }
-    __device__ uint32_t pos(int64_t i) const { return p[i]; }
+    const Pair* p;
+    __device__ uint32_t key(int64_t i) const { return p[i].key; }
+    __device__ Pair pair(int64_t i) const { return p[i]; }
 };
 
 // Fills this worker's share of the table's bytes with zeros.
@@ -173,91 +176,102 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[J], const boo
     }
 }
 
-// One workgroup sorts everything (n, the padded length, is at most 1,024 J): keys and positions stay in registers, each pass exchanges them
-// through LDS.  The launch's other workgroups fill zeros.
-constexpr int kSortThreads = 1024;
-constexpr int kSortWaves = kSortThreads / 64;
+// Short lists, in two launches without passes.  k_sort_tiles orders tiles of 256 entries, an entry's place being the
+// number of entries of its tile before it, counted: each wave compares 64 entries, one to a lane, with 64 others.
+// k_sort_merge then places every entry in the whole list: its place is the sum over the tiles of the entries before it,
+// which a binary search in each finds (those of equal key count in the tiles before its own).  A workgroup of
+// k_sort_merge holds all keys in LDS and places 64 entries, one to a lane; each of its waves searches a
+// sixteenth of the tiles, four at a time.
+constexpr int kSmallTile = 256;
+constexpr int kMergeThreads = 1024;
+constexpr int kMergeWaves = kMergeThreads / 64;
 
-template <int J>
-constexpr size_t sort_one_lds(int bins) {
-    return (size_t)kSortThreads * J * 6 + (size_t)kSortWaves * bins * 2 + 64 * 4;
-}
-
-template <int J, typename TI>
-__global__ void __launch_bounds__(kSortThreads) k_sort_one(Tokens<TI> src, uint32_t n, int passes, int bits, uint32_t* __restrict__ keys,
-                                                           uint32_t* __restrict__ pos, Fill fill) {
-    if (blockIdx.x) {
-        fill_zero(fill, blockIdx.x - 1, gridDim.x - 1);
+template <typename TI>
+__global__ void __launch_bounds__(4 * kSmallTile) k_sort_tiles(Tokens<TI> src, uint32_t n, Pair* __restrict__ pairs, uint32_t tiles, Fill fill) {
+    if (blockIdx.x >= tiles) {
+        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
         return;
     }
-    extern __shared__ __align__(16) char lds[];
-    const int bins = 1 << bits;
-    uint32_t* const lkey = reinterpret_cast<uint32_t*>(lds);
-    uint16_t* const lpos = reinterpret_cast<uint16_t*>(lkey + kSortThreads * J);
-    uint16_t* const counts = lpos + kSortThreads * J;  // [waves][bins]
-    uint32_t* const sums = reinterpret_cast<uint32_t*>(counts + kSortWaves * bins);
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = wave * 64 * J + lane;
-    uint32_t key[J], place[J], digit[J], rank[J];
-    bool on[J];
+    __shared__ __align__(16) uint32_t keys[kSmallTile];
+    __shared__ uint32_t counts[4][kSmallTile];
+    const uint32_t at = threadIdx.x % kSmallTile, part = threadIdx.x / kSmallTile, own = at / 64;
+    const uint32_t i = blockIdx.x * kSmallTile + at;
+    const Pair p = src.pair(i);
+    if (part == 0) keys[at] = i < n ? p.key : 0xFFFFFFFFu;  // above every key
+    __syncthreads();
+    uint32_t before = 0;
+    if (part == own) {
+#pragma unroll 8
+        for (uint32_t k = 0; k < 64; ++k) {
+            const uint32_t q = keys[part * 64 + k];
+            before += q < p.key || (q == p.key && k < at % 64);
+        }
+    } else {
+        const uint32_t bound = p.key + (part < own);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const uint32_t i = at + j * 64;
-        on[j] = i < n;
-        key[j] = src.key(i);
-        place[j] = src.pos(i);
+        for (uint32_t k = 0; k < 16; ++k) {
+            const uint4 q = reinterpret_cast<const uint4*>(keys + part * 64)[k];
+            before += (q.x < bound) + (q.y < bound) + (q.z < bound) + (q.w < bound);
+        }
     }
-    for (int p = 0; p < passes; ++p) {
-        for (int i = threadIdx.x; i < kSortWaves * bins / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < J; ++j) digit[j] = (key[j] >> (p * bits)) & (uint32_t)(bins - 1);
-        wave_ranks<J>(digit, on, bits, counts + wave * bins, rank);
-        __syncthreads();
-        // Digit-major, wave-minor prefix sums of the counts (bins <= the threads).
-        uint32_t c[kSortWaves], sum = 0, total;
-        const bool mine = threadIdx.x < (uint32_t)bins;
-#pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) {
-            c[w] = mine ? counts[w * bins + threadIdx.x] : 0;
-            sum += c[w];
-        }
-        uint32_t base = block_exclusive(sum, sums, total);
-#pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) {
-            if (mine) counts[w * bins + threadIdx.x] = (uint16_t)base;
-            base += c[w];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (on[j]) {
-                const uint32_t to = counts[wave * bins + digit[j]] + rank[j];
-                lkey[to] = key[j];
-                lpos[to] = (uint16_t)place[j];
-            }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            key[j] = lkey[at + j * 64];
-            place[j] = lpos[at + j * 64];
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-        if (on[j]) {
-            keys[at + j * 64] = key[j];
-            pos[at + j * 64] = place[j];
-        }
+    counts[part][at] = before;
+    __syncthreads();
+    if (part == 0 && i < n) pairs[blockIdx.x * kSmallTile + counts[0][at] + counts[1][at] + counts[2][at] + counts[3][at]] = p;
 }
 
-// Many workgroups: a tile of kTile consecutive keys each; per pass the tiles' digit counts (k_sort_count),
-// their prefix sums along each digit (k_sort_scan), and the move (k_sort_move).  Each launch fills a part of the
-// zeros with extra workgroups.
+__global__ void __launch_bounds__(kMergeThreads) k_sort_merge(const Pair* __restrict__ in, uint32_t n, Pair* __restrict__ out,
+                                                              uint32_t own_blocks, Fill fill) {
+    if (blockIdx.x >= own_blocks) {
+        fill_zero(fill, blockIdx.x - own_blocks, gridDim.x - own_blocks);
+        return;
+    }
+    constexpr int U = 4;
+    extern __shared__ __align__(16) uint32_t keys[];  // whole tiles, then a count per wave and entry
+    const uint32_t tiles = (n + kSmallTile - 1) / kSmallTile, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    uint32_t* const counts = keys + tiles * kSmallTile;
+    const uint32_t i = blockIdx.x * 64 + lane, own = i / kSmallTile;
+    const Pair p = in[min(i, n - 1)];
+    for (uint32_t k = threadIdx.x; k < tiles * kSmallTile; k += kMergeThreads) keys[k] = k < n ? in[k].key : 0xFFFFFFFFu;
+    __syncthreads();
+    uint32_t before = 0;
+    for (uint32_t t = wave; t < tiles; t += U * kMergeWaves) {
+        uint32_t at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) at[u] = 0;
+#pragma unroll
+        for (uint32_t step = kSmallTile / 2; step; step /= 2)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t q = min(t + u * kMergeWaves, tiles - 1);
+                at[u] += keys[q * kSmallTile + at[u] + step - 1] < p.key + (q < own) ? step : 0;
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t q = t + u * kMergeWaves;
+            if (q >= tiles || q == own) continue;
+            before += at[u] + (keys[q * kSmallTile + at[u]] < p.key + (q < own));
+        }
+    }
+    counts[wave * 64 + lane] = before;
+    __syncthreads();
+    if (wave == 0 && i < n) {
+        uint32_t to = i % kSmallTile;
+#pragma unroll
+        for (int w = 0; w < kMergeWaves; ++w) to += counts[w * 64 + lane];
+        out[to] = p;
+    }
+}
+
+// Long lists: a radix sort from the lowest digit up, a workgroup for each tile of kTile consecutive entries.  A pass
+// counts the tiles' digits (k_sort_count), sums the counts along the tiles (k_sort_scan), and moves the entries
+// (k_sort_move), which orders its tile in LDS first, so that it writes runs of consecutive entries.  Every launch
+// fills a part of the zeros with further workgroups.
 constexpr int kTileThreads = 512;
 constexpr int kTileJ = 8;
 constexpr int kTile = kTileThreads * kTileJ;
+constexpr int kTileWaves = kTileThreads / 64;
 constexpr int kMaxBits = 11;
+constexpr int kPer = (1 << kMaxBits) / kTileThreads;  // digits a thread at most: k_sort_move gives it consecutive ones
 
 template <typename SRC>
 __global__ void __launch_bounds__(kTileThreads) k_sort_count(SRC src, int64_t n, int shift, int bits, uint32_t tiles,
@@ -267,108 +281,142 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_count(SRC src, int64_t n,
         return;
     }
     __shared__ uint32_t count[1 << kMaxBits];
-    const int bins = 1 << bits;
-    for (int i = threadIdx.x; i < bins; i += kTileThreads) count[i] = 0;
+    const uint32_t bins = 1u << bits;
+    for (uint32_t d = threadIdx.x; d < bins; d += kTileThreads) count[d] = 0;
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * kTile;
 #pragma unroll
     for (int j = 0; j < kTileJ; ++j) {
         const int64_t i = base + j * kTileThreads + threadIdx.x;
-        if (i < n) atomicAdd(&count[(src.key(i) >> shift) & (uint32_t)(bins - 1)], 1u);
+        if (i < n) atomicAdd(&count[(src.key(i) >> shift) & (bins - 1)], 1u);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < bins; i += kTileThreads) hist[(int64_t)i * tiles + blockIdx.x] = count[i];
+    for (uint32_t d = threadIdx.x; d < bins; d += kTileThreads) hist[((int64_t)blockIdx.x << bits) + d] = count[d];
 }
 
-// One wave per digit: hist[digit][tile] becomes the digit's count in the tiles before, totals[digit] in all.
-__global__ void __launch_bounds__(kThreads) k_sort_scan(uint32_t* __restrict__ hist, uint32_t tiles, uint32_t bins,
-                                                        uint32_t* __restrict__ totals, Fill fill) {
-    const uint32_t scans = (bins + kThreads / 64 - 1) / (kThreads / 64);
-    if (blockIdx.x >= scans) {
-        fill_zero(fill, blockIdx.x - scans, gridDim.x - scans);
+// hist[tile][digit] becomes the digit's count in the tiles before, totals[digit] its count in all: kScanDigits digits a
+// workgroup, the tiles in kScanSlices runs.
+constexpr int kScanDigits = 16;
+constexpr int kScanSlices = 64;
+
+__global__ void __launch_bounds__(kScanDigits * kScanSlices) k_sort_scan(uint32_t* __restrict__ hist, uint32_t tiles, int bits,
+                                                                uint32_t* __restrict__ totals, uint32_t own_blocks, Fill fill) {
+    if (blockIdx.x >= own_blocks) {
+        fill_zero(fill, blockIdx.x - own_blocks, gridDim.x - own_blocks);
         return;
     }
-    const uint32_t lane = threadIdx.x % 64, d = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    if (d >= bins) return;
-    uint32_t* const h = hist + (int64_t)d * tiles;
-    uint32_t before = 0;
-    for (uint32_t t = 0; t < tiles; t += 64) {
-        const uint32_t x = t + lane < tiles ? h[t + lane] : 0;
-        uint32_t s = x;
+    constexpr int U = 8;
+    __shared__ uint32_t sums[kScanSlices][kScanDigits];
+    const uint32_t lane = threadIdx.x % kScanDigits, slice = threadIdx.x / kScanDigits, d = blockIdx.x * kScanDigits + lane;
+    const bool on = d < 1u << bits;
+    const uint32_t t0 = (uint32_t)((uint64_t)tiles * slice / kScanSlices), t1 = (uint32_t)((uint64_t)tiles * (slice + 1) / kScanSlices);
+    uint32_t x[U], sum = 0;
+    const auto fetch = [&](uint32_t t) {
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t y = __shfl_up(s, o);
-            if (lane >= (uint32_t)o) s += y;
-        }
-        if (t + lane < tiles) h[t + lane] = before + s - x;
-        before += __shfl(s, 63);
+        for (int u = 0; u < U; ++u) x[u] = on && t + u < t1 ? hist[((int64_t)(t + u) << bits) + d] : 0;
+    };
+    for (uint32_t t = t0; t < t1; t += U) {
+        fetch(t);
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum += x[u];
     }
-    if (lane == 0) totals[d] = before;
+    sums[slice][lane] = sum;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
+#pragma unroll 16
+    for (uint32_t k = 0; k < kScanSlices; ++k) {
+        const uint32_t y = sums[k][lane];
+        before += k < slice ? y : 0;
+        total += y;
+    }
+    for (uint32_t t = t0; t < t1; t += U) {
+        if (t1 - t0 > U) fetch(t);  // a run of up to U tiles is still there
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (on && t + u < t1) {
+                hist[((int64_t)(t + u) << bits) + d] = before;
+                before += x[u];
+            }
+    }
+    if (on && slice == 0) totals[d] = total;
 }
 
 template <typename SRC>
 __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, int shift, int bits, uint32_t tiles,
                                                             const uint32_t* __restrict__ hist,
-                                                            const uint32_t* __restrict__ totals,
-                                                            uint32_t* __restrict__ keys, uint32_t* __restrict__ pos, Fill fill) {
+                                                            const uint32_t* __restrict__ totals, Pair* __restrict__ out, Fill fill) {
     if (blockIdx.x >= tiles) {
         fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
         return;
     }
-    constexpr int kWaves = kTileThreads / 64;
-    constexpr int kPer = (1 << kMaxBits) / kTileThreads;
-    __shared__ uint16_t counts[kWaves << kMaxBits];
-    __shared__ uint32_t start[1 << kMaxBits];
-    __shared__ uint32_t sums[kWaves];
-    const int bins = 1 << bits;
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int i = threadIdx.x; i < kWaves * bins; i += kTileThreads) counts[i] = 0;
-    // Where each digit's keys of this tile begin: the smaller digits' totals and the tiles before.
-    uint32_t t[kPer], sum = 0, total;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const int d = (int)threadIdx.x * kPer + k;
-        t[k] = d < bins ? totals[d] : 0;
-        sum += t[k];
-    }
-    uint32_t base = block_exclusive(sum, sums, total);
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const int d = (int)threadIdx.x * kPer + k;
-        if (d < bins) start[d] = base + hist[(int64_t)d * tiles + blockIdx.x];
-        base += t[k];
-    }
-    const int64_t at = (int64_t)blockIdx.x * kTile + wave * 64 * kTileJ + lane;
-    uint32_t key[kTileJ], place[kTileJ], digit[kTileJ], rank[kTileJ];
+    __shared__ Pair tile[kTile];
+    extern __shared__ __align__(16) uint32_t shift_of[];              // [digit]: from a place in the ordered tile to that in `out`
+    uint16_t* const counts = reinterpret_cast<uint16_t*>(shift_of + (1 << bits));  // [wave][digit]
+    __shared__ uint32_t sums[kTileWaves];
+    const uint32_t bins = 1u << bits, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint32_t per = max(1u, bins / kTileThreads), d0 = threadIdx.x * per;
+    for (uint32_t i = threadIdx.x; i < kTileWaves * bins / 2; i += kTileThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
+    const int64_t base = (int64_t)blockIdx.x * kTile, at = base + wave * 64 * kTileJ + lane;
+    Pair p[kTileJ];
+    uint32_t digit[kTileJ], rank[kTileJ], all = 0, total;
     bool on[kTileJ];
 #pragma unroll
     for (int j = 0; j < kTileJ; ++j) {
         const int64_t i = at + j * 64;
         on[j] = i < n;
-        key[j] = on[j] ? src.key(i) : 0;
-        place[j] = on[j] ? src.pos(i) : 0;
-        digit[j] = (key[j] >> shift) & (uint32_t)(bins - 1);
+        p[j] = src.pair(on[j] ? i : 0);
+        digit[j] = (p[j].key >> shift) & (bins - 1);
     }
-    __syncthreads();
+    // Where the digits of this thread begin in `out`: the smaller digits' totals and the tiles before.
+    uint32_t t[kPer], earlier[kPer];
+#pragma unroll
+    for (uint32_t k = 0; k < kPer; ++k) {
+        const bool mine = k < per && d0 + k < bins;
+        t[k] = mine ? totals[d0 + k] : 0;
+        earlier[k] = mine ? hist[((int64_t)blockIdx.x << bits) + d0 + k] : 0;
+        all += t[k];
+    }
+    uint32_t start = block_exclusive(all, sums, total);
     wave_ranks<kTileJ>(digit, on, bits, counts + wave * bins, rank);
     __syncthreads();
-    for (int d = threadIdx.x; d < bins; d += kTileThreads) {
-        uint32_t b = 0;
+    uint32_t here[kPer], sum = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const uint32_t c = counts[w * bins + d];
-            counts[w * bins + d] = (uint16_t)b;
-            b += c;
-        }
+    for (uint32_t k = 0; k < kPer; ++k) {
+        here[k] = 0;
+        if (k < per && d0 + k < bins)
+#pragma unroll
+            for (int w = 0; w < kTileWaves; ++w) here[k] += counts[w * bins + d0 + k];
+        sum += here[k];
     }
+    uint32_t first = block_exclusive(sum, sums, total);
+#pragma unroll
+    for (uint32_t k = 0; k < kPer; ++k)
+        if (k < per && d0 + k < bins) {
+            shift_of[d0 + k] = start + earlier[k] - first;
+            start += t[k];
+            uint32_t to = first;
+#pragma unroll
+            for (int w = 0; w < kTileWaves; ++w) {
+                const uint32_t c = counts[w * bins + d0 + k];
+                counts[w * bins + d0 + k] = (uint16_t)to;
+                to += c;
+            }
+            first = to;
+        }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kTileJ; ++j)
-        if (on[j]) {
-            const uint32_t to = start[digit[j]] + counts[wave * bins + digit[j]] + rank[j];
-            keys[to] = key[j];
-            pos[to] = place[j];
+        if (on[j]) tile[counts[wave * bins + digit[j]] + rank[j]] = p[j];
+    __syncthreads();
+    const uint32_t entries = (uint32_t)min((int64_t)kTile, n - base);
+#pragma unroll
+    for (int j = 0; j < kTileJ; ++j) {
+        const uint32_t i = j * kTileThreads + threadIdx.x;
+        if (i < entries) {
+            const Pair q = tile[i];
+            out[i + shift_of[(q.key >> shift) & (bins - 1)]] = q;
         }
+    }
 }
 
 // ---------------------------------------------------------------------------------------- sums
@@ -377,8 +425,7 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
 // them in order.  All pieces are 32 bits and unscaled.
 
 struct SumArgs {
-    const uint32_t* keys;
-    const uint32_t* pos;
+    const Pair* pairs;
     int64_t n;
     uint32_t share;  // S
     uint32_t rows;
@@ -421,24 +468,24 @@ __global__ void __launch_bounds__(kThreads) k_sums(SumArgs a, const TG* __restri
     if (e0 >= a.n || col * VEC >= a.dim) return;
     int32_t again;
     const int32_t c = vec_column<VEC>(col, a.dim, again);
-    uint32_t cur = a.keys[e0];
-    bool cut = e0 > 0 && a.keys[e0 - 1] == cur;
+    uint32_t cur = a.pairs[e0].key;
+    bool cut = e0 > 0 && a.pairs[e0 - 1].key == cur;
     float acc[VEC] = {};
     for (int64_t e = e0; e < e1; e += U) {
-        const Raw<U, uint32_t> k = load_raw<U>(a.keys + e), p = load_raw<U>(a.pos + e);
+        const Raw<U, Pair> p = load_raw<U>(a.pairs + e);
         Raw<VEC, TG> v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            v[u] = load_raw<VEC>(grad + (int64_t)p.t[u] * a.gstride + c);
+            v[u] = load_raw<VEC>(grad + (int64_t)p.t[u].pos * a.gstride + c);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (k.t[u] != cur) {
+            if (p.t[u].key != cur) {
                 if (cut)
                     store_vec(a.head + g * a.dim + c, acc);
                 else
                     write_row<VEC, ACC>(a, out, cur, c, again, acc);
                 cut = false;
-                cur = k.t[u];
+                cur = p.t[u].key;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
             }
@@ -449,7 +496,7 @@ __global__ void __launch_bounds__(kThreads) k_sums(SumArgs a, const TG* __restri
         }
     }
     if (cur >= a.rows) return;
-    if (e1 < a.n && a.keys[e1] == cur)
+    if (e1 < a.n && a.pairs[e1].key == cur)
         store_vec(a.tail + g * a.dim + c, acc);
     else if (cut)
         store_vec(a.head + g * a.dim + c, acc);
@@ -473,28 +520,63 @@ __device__ __forceinline__ void add_tails(const SumArgs& a, int64_t first, int64
     }
 }
 
-// The group (at most g) in which the run that ends in group g begins.
+// The group in which the run that covers the start of group g (and the entry before it) begins.  The starts of the
+// groups 1, 2, 4, ... before are looked at, several together, then the range between two of them in eighths.
 __device__ __forceinline__ int64_t run_begins(const SumArgs& a, int64_t g, uint32_t row) {
-    int64_t lo = 0, hi = g * a.share;  // keys[hi] == row
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (a.keys[mid] < row)
-            lo = mid + 1;
-        else
-            hi = mid;
+    constexpr int P = 8;
+    const auto covers = [&](int64_t k, uint32_t key) { return k > 0 && key == row; };
+    const auto before = [&](int64_t k) { return a.pairs[max(k, (int64_t)1) * a.share - 1].key; };
+    int64_t in = g, out = 0;  // the run covers the start of `in`; once out < in, not that of `out`
+    bool more = true;
+    const auto probe = [&](auto probes, int64_t step) {  // looks at g - step, g - 2 step, g - 4 step, ... together
+        constexpr int N = decltype(probes)::value;
+        uint32_t key[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) key[i] = before(g - (step << i));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t k = g - (step << i);
+            if (more && covers(k, key[i])) {
+                in = k;
+            } else if (more) {
+                out = max(k, (int64_t)0);
+                more = false;
+            }
+        }
+    };
+    probe(Int<2>{}, 1);  // most runs are short
+    int64_t step = 4;
+    while (more) {
+        probe(Int<P>{}, step);
+        step <<= P;
     }
-    return lo / a.share;
+    while (in - out > 1) {  // the run's first entry lies in a group from `out` to in - 1
+        const int64_t lo = out, size = in - out;
+        uint32_t key[P - 1];
+#pragma unroll
+        for (int i = 1; i < P; ++i) key[i - 1] = before(lo + max((int64_t)1, size * i / P));
+#pragma unroll
+        for (int i = P - 1; i >= 1; --i) {
+            const int64_t k = lo + max((int64_t)1, size * i / P);
+            if (covers(k, key[i - 1])) in = min(in, k);
+        }
+#pragma unroll
+        for (int i = 1; i < P; ++i) {
+            const int64_t k = lo + max((int64_t)1, size * i / P);
+            if (!covers(k, key[i - 1])) out = max(out, k);
+        }
+    }
+    return out;
 }
 
-// Rows cut into at most kShortRun pieces are joined by their group; longer ones then by the whole workgroup, group j
-// taking every m-th piece from the j-th on and the m sums added in order.
-constexpr int kShortRun = 16;
-
-template <int VEC, bool ACC, typename TO>
-__global__ void __launch_bounds__(kThreads) k_sums_join(SumArgs a, TO* __restrict__ out, uint32_t log2_lanes) {
-    __shared__ float part[kThreads * VEC];
-    __shared__ int64_t ends[kThreads], begins[kThreads];
-    const uint32_t m = kThreads >> log2_lanes, j = threadIdx.x >> log2_lanes, l = threadIdx.x & ((1u << log2_lanes) - 1);
+// A row's pieces are joined by their last group where they are few.  Of more pieces, each of the m groups of a wave (or,
+// where a wave has one group or the run is very long, of the workgroup) adds every m-th, and the m sums are added in
+// a fixed order.
+template <int VEC, bool ACC, int THREADS, typename TO>
+__global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict__ out, uint32_t log2_lanes) {
+    __shared__ float part[THREADS * VEC];
+    __shared__ int64_t ends[THREADS], begins[THREADS];
+    const uint32_t m = THREADS >> log2_lanes, j = threadIdx.x >> log2_lanes, l = threadIdx.x & ((1u << log2_lanes) - 1);
     const int64_t g = (int64_t)blockIdx.x * m + j;
     const int32_t col = (int32_t)((blockIdx.y << log2_lanes) + l);
     const bool in = col * VEC < a.dim;
@@ -504,20 +586,38 @@ __global__ void __launch_bounds__(kThreads) k_sums_join(SumArgs a, TO* __restric
     int64_t begin = -1;
     uint32_t row = 0;
     if (e0 > 0 && e0 < a.n) {
-        row = a.keys[e0];
-        if (row < a.rows && a.keys[e0 - 1] == row && (e1 == a.n || a.keys[e1] != row)) begin = run_begins(a, g, row);
+        const uint32_t before = a.pairs[e0 - 1].key, after = a.pairs[min(e1, a.n - 1)].key;
+        row = a.pairs[e0].key;
+        if (row < a.rows && before == row && (e1 == a.n || after != row)) begin = run_begins(a, g, row);
     }
-    const bool is_long = begin >= 0 && g - begin > kShortRun;
+    const int64_t pieces = begin >= 0 ? g - begin : 0;
+    const uint32_t beside = log2_lanes < 6 ? 64 >> log2_lanes : 1;  // groups in a wave
+    const bool is_long = pieces > (beside > 1 ? 32 * beside : 16), is_wave = !is_long && beside > 1 && pieces > 16;
     if (l == 0) {
         ends[j] = is_long ? g : -1;
         begins[j] = begin;
     }
-    if (begin >= 0 && !is_long && in) {
-        float s[VEC] = {}, h[VEC];
-        add_tails<VEC>(a, begin, g, 1, c, s);
-        load_vec(a.head + g * a.dim + c, h);
+    for (uint64_t todo = __ballot(is_wave && l == 0); todo; todo &= todo - 1) {
+        const int at = __builtin_ctzll(todo);
+        const int64_t last = __shfl((int)g, at), from = __shfl((int)begin, at);
+        float s[VEC] = {};
+        if (in) add_tails<VEC>(a, from + j % beside, last, beside, c, s);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) s[i] += h[i];
+        for (int i = 0; i < VEC; ++i)
+            for (int o = 32; o >= 1 << log2_lanes; o /= 2) s[i] += __shfl_xor(s[i], o);
+        if (g == last && in) {
+            const Raw<VEC, float> h = load_raw<VEC>(a.head + g * a.dim + c);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s[i] += h.t[i];
+            write_row<VEC, ACC>(a, out, row, c, again, s);
+        }
+    }
+    if (begin >= 0 && !is_long && !is_wave && in) {
+        float s[VEC] = {};
+        const Raw<VEC, float> h = load_raw<VEC>(a.head + g * a.dim + c);
+        add_tails<VEC>(a, begin, g, 1, c, s);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[i] += h.t[i];
         write_row<VEC, ACC>(a, out, row, c, again, s);
     }
     __syncthreads();
@@ -537,7 +637,7 @@ __global__ void __launch_bounds__(kThreads) k_sums_join(SumArgs a, TO* __restric
             load_vec(a.head + end * a.dim + c, h);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s[i] += h[i];
-            write_row<VEC, ACC>(a, out, a.keys[end * a.share], c, again, s);
+            write_row<VEC, ACC>(a, out, a.pairs[end * a.share].key, c, again, s);
         }
         __syncthreads();
     }
@@ -568,61 +668,78 @@ bool is_token(int32_t t) { return t == SCD_I32 || t == SCD_I64; }
 // How a gradient call sorts and splits: a function of the sizes alone.
 struct Plan {
     int64_t n;        // padded to whole batches
-    bool one;         // one workgroup sorts
+    bool tiled;       // a short list
     int passes, bits;
     int64_t tiles;
     uint32_t share;
     int64_t groups;
-    int64_t pairs;    // bytes of one key or position array
+    int64_t pairs;    // bytes of one list
     int64_t hist, pieces, bytes;
 };
 
-constexpr int64_t kSortOneMax = int64_t(kSortThreads) * 16;
+constexpr int64_t kTiledMax = 16384;
 
 int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
 
 Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     Plan p{};
     p.n = ceil_div(n, kBatch) * kBatch;
-    p.one = p.n <= kSortOneMax;
-    const int key_bits = (int)log2_up((uint64_t)rows + 1);
-    const int most = p.one ? 9 : kMaxBits;
-    p.passes = std::max(1, (key_bits + most - 1) / most);
-    p.bits = std::max(1, (key_bits + p.passes - 1) / p.passes);
-    p.tiles = p.one ? 0 : ceil_div(p.n, kTile);
+    p.tiled = p.n <= kTiledMax;
+    const int key_bits = std::max(1, (int)log2_up((uint64_t)rows + 1));
+    // Digits of 9 bits, or of up to 11 where that saves a pass: the more digits, the shorter the runs that a tile writes.
+    p.passes = std::min((key_bits + 8) / 9, (key_bits + kMaxBits - 1) / kMaxBits);
+    p.bits = (key_bits + p.passes - 1) / p.passes;
+    p.tiles = ceil_div(p.n, kTile);
     // Entries per group: as many as keep about 4,096 waves in work, 8 at least, 64 at most.
     const int64_t work = p.n * ceil_div(dim, 4) / 64;
     p.share = (uint32_t)std::min<int64_t>(64, std::max<int64_t>(8, work / 4096 / 8 * 8));
     p.groups = ceil_div(p.n, p.share);
-    p.pairs = p.n * 4;
-    p.hist = p.one ? 0 : align16(((p.tiles + 1) << p.bits) * 4);
+    p.pairs = align16(p.n * sizeof(Pair));
+    p.hist = p.tiled ? 0 : align16(((p.tiles + 1) << p.bits) * 4);
     p.pieces = align16(p.groups * dim * 4);
-    p.bytes = (p.one ? 2 : 4) * p.pairs + p.hist + 2 * p.pieces;
+    p.bytes = 2 * p.pairs + p.hist + 2 * p.pieces;
     return p;
 }
 
-// Workgroups of `threads` threads that fill a part of the zeros beside other work: 64 KB each, at most as many as the
-// GPU has CUs (a few each where the others are small).
+// Workgroups of `threads` threads that fill a part of the zeros beside other work: 64 bytes a thread, up to eight waves
+// for each of the GPU's SIMDs.
 uint32_t fill_blocks(const Fill& f, int threads) {
     if (!f.p) return 0;
-    return (uint32_t)std::min<int64_t>(ceil_div(f.rows * f.row_bytes, 65536), 255 * (1024 / threads));
+    return (uint32_t)std::min<int64_t>(ceil_div(f.rows * f.row_bytes, threads * 64), 512 * (1024 / threads));
 }
 
-template <int J, typename TI>
-int launch_sort_one(Tokens<TI> src, const Plan& p, uint32_t* keys, uint32_t* pos, const Fill& fill, hipStream_t s) {
-    const size_t lds = sort_one_lds<J>(1 << p.bits);
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_one<J, TI>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return fail(SCD_ERR_HIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-    k_sort_one<J, TI><<<1 + fill_blocks(fill, kSortThreads), kSortThreads, lds, s>>>(src, (uint32_t)p.n, p.passes, p.bits, keys, pos, fill);
+// The first `part` of `parts` equal parts, the second, ...
+Fill fill_part(const Fill& f, int64_t part, int64_t parts) {
+    const int64_t a = f.rows * part / parts, b = f.rows * (part + 1) / parts;
+    return f.p && b > a ? Fill{f.p + a * f.stride, b - a, f.row_bytes, f.stride} : Fill{};
+}
+
+// Leaves the sorted list in `pairs`; `other` is scratch.
+template <typename TI>
+int sort_short(Tokens<TI> src, const Plan& p, Pair* pairs, Pair* other, const Fill& fill, hipStream_t s) {
+    const uint32_t tiles = (uint32_t)ceil_div(p.n, kSmallTile), blocks = (uint32_t)ceil_div(p.n, 64);
+    const int launches = tiles > 1 ? 2 : 1;
+    Fill part = fill_part(fill, 0, launches);
+    k_sort_tiles<<<tiles + fill_blocks(part, 4 * kSmallTile), 4 * kSmallTile, 0, s>>>(src, (uint32_t)p.n, launches > 1 ? other : pairs, tiles, part);
+    if (launches > 1) {
+        const size_t lds = (size_t)(tiles * kSmallTile + kMergeThreads) * 4;
+        if (lds > 65536) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_merge), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return fail(SCD_ERR_HIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
+        }
+        part = fill_part(fill, 1, launches);
+        k_sort_merge<<<blocks + fill_blocks(part, kMergeThreads), kMergeThreads, lds, s>>>(other, (uint32_t)p.n, pairs, blocks, part);
+    }
     return launched("sort of tokens");
 }
 
 template <typename SRC>
-void launch_pass(SRC src, int pass, const Plan& p, uint32_t* hist, uint32_t* totals, uint32_t* keys, uint32_t* pos, Fill* fills, hipStream_t s) {
-    const uint32_t tiles = (uint32_t)p.tiles, bins = 1u << p.bits;
-    k_sort_count<<<tiles + fill_blocks(fills[0], kTileThreads), kTileThreads, 0, s>>>(src, p.n, pass * p.bits, p.bits, tiles, hist, fills[0]);
-    k_sort_scan<<<(uint32_t)ceil_div(bins, kThreads / 64) + fill_blocks(fills[1], kThreads), kThreads, 0, s>>>(hist, tiles, bins, totals, fills[1]);
-    k_sort_move<<<tiles + fill_blocks(fills[2], kTileThreads), kTileThreads, 0, s>>>(src, p.n, pass * p.bits, p.bits, tiles, hist, totals, keys, pos, fills[2]);
+void launch_pass(SRC src, int pass, const Plan& p, uint32_t* hist, uint32_t* totals, Pair* out, const Fill* fills, hipStream_t s) {
+    const uint32_t tiles = (uint32_t)p.tiles, scans = (uint32_t)ceil_div(1 << p.bits, kScanDigits);
+    const int shift = pass * p.bits;
+    k_sort_count<<<tiles + fill_blocks(fills[0], kTileThreads), kTileThreads, 0, s>>>(src, p.n, shift, p.bits, tiles, hist, fills[0]);
+    k_sort_scan<<<scans + fill_blocks(fills[1], kScanDigits * kScanSlices), kScanDigits * kScanSlices, 0, s>>>(hist, tiles, p.bits, totals, scans, fills[1]);
+    k_sort_move<<<tiles + fill_blocks(fills[2], kTileThreads), kTileThreads, (4 + 2 * kTileWaves) << p.bits, s>>>(src, p.n, shift, p.bits, tiles, hist, totals, out, fills[2]);
 }
 
 }  // namespace
@@ -692,44 +809,29 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
     if (n > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < p.bytes))
         return fail(SCD_ERR_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)p.bytes);
     char* w = (char*)workspace;
-    uint32_t* keys = (uint32_t*)w;
-    uint32_t* pos = (uint32_t*)(w + p.pairs);
+    Pair* pairs = (Pair*)w;
     int rc = SCD_OK;
     const auto sort = [&](auto ti) {
         using TI = decltype(ti);
         const Tokens<TI> src{(const TI*)tokens, n, (uint32_t)rows};
-        if (p.one) {
-            if (p.n <= kSortThreads)
-                rc = launch_sort_one<1>(src, p, keys, pos, fill, s);
-            else if (p.n <= 4 * kSortThreads)
-                rc = launch_sort_one<4>(src, p, keys, pos, fill, s);
-            else
-                rc = launch_sort_one<16>(src, p, keys, pos, fill, s);
+        Pair* const other = (Pair*)(w + p.pairs);
+        if (p.tiled) {
+            rc = sort_short(src, p, pairs, other, fill, s);
             return;
         }
         // The passes' launches share the zeros evenly.
-        uint32_t* const other_keys = (uint32_t*)(w + 2 * p.pairs);
-        uint32_t* const other_pos = (uint32_t*)(w + 3 * p.pairs);
-        uint32_t* const hist = (uint32_t*)(w + 4 * p.pairs);
+        uint32_t* const hist = (uint32_t*)(w + 2 * p.pairs);
         uint32_t* const totals = hist + (p.tiles << p.bits);
         const int launches = 3 * p.passes;
         for (int k = 0; k < p.passes; ++k) {
-            Fill part[3] = {};
-            for (int j = 0; fill.p && j < 3; ++j) {
-                const int64_t a = rows * (3 * k + j) / launches, b = rows * (3 * k + j + 1) / launches;
-                if (b > a) part[j] = Fill{fill.p + a * fill.stride, b - a, fill.row_bytes, fill.stride};
-            }
-            uint32_t* const to_keys = k % 2 ? other_keys : keys;
-            uint32_t* const to_pos = k % 2 ? other_pos : pos;
+            const Fill part[3] = {fill_part(fill, 3 * k, launches), fill_part(fill, 3 * k + 1, launches), fill_part(fill, 3 * k + 2, launches)};
+            Pair* const to = k % 2 ? other : pairs;
             if (k == 0)
-                launch_pass(src, k, p, hist, totals, to_keys, to_pos, part, s);
+                launch_pass(src, k, p, hist, totals, to, part, s);
             else
-                launch_pass(Pairs{k % 2 ? keys : other_keys, k % 2 ? pos : other_pos}, k, p, hist, totals, to_keys, to_pos, part, s);
+                launch_pass(Pairs{k % 2 ? pairs : other}, k, p, hist, totals, to, part, s);
         }
-        if (p.passes % 2 == 0) {
-            keys = other_keys;
-            pos = other_pos;
-        }
+        if (p.passes % 2 == 0) pairs = other;
         rc = launched("sort of tokens");
     };
     if (token_type == SCD_I32)
@@ -738,8 +840,7 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         sort(int64_t{});
     if (rc != SCD_OK || n == 0) return rc;
     SumArgs a{};
-    a.keys = keys;
-    a.pos = pos;
+    a.pairs = pairs;
     a.n = p.n;
     a.share = p.share;
     a.rows = (uint32_t)rows;
@@ -747,7 +848,7 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
     a.scale = scale;
     a.gstride = grad_stride;
     a.ostride = rows > 1 ? out_stride : dim;
-    a.head = (float*)(w + (p.one ? 2 : 4) * p.pairs + p.hist);
+    a.head = (float*)(w + 2 * p.pairs + p.hist);
     a.tail = (float*)((char*)a.head + p.pieces);
     with_vec(grad_type, out_type, dim, [&](auto tg, auto to, auto vc) {
         using TG = decltype(tg);
@@ -758,7 +859,13 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         const auto go = [&](auto acc) {
             constexpr bool ACC = decltype(acc)::value;
             k_sums<VEC, ACC><<<grid, kThreads, 0, s>>>(a, (const TG*)grad, (TO*)out, m.log2_lanes);
-            if (p.groups > 1) k_sums_join<VEC, ACC><<<grid, kThreads, 0, s>>>(a, (TO*)out, m.log2_lanes);
+            const auto join = [&](auto threads) {
+                constexpr int THREADS = decltype(threads)::value;
+                const dim3 blocks((uint32_t)ceil_div(p.groups, THREADS >> m.log2_lanes), m.ranges);
+                k_sums_join<VEC, ACC, THREADS><<<blocks, THREADS, 0, s>>>(a, (TO*)out, m.log2_lanes);
+            };
+            // Wide rows get workgroups of several groups all the same.
+            if (p.groups > 1) m.log2_lanes >= 6 ? join(Int<1024>{}) : join(Int<kThreads>{});
         };
         accumulate ? go(std::true_type{}) : go(std::false_type{});
     });

@@ -377,6 +377,8 @@ bool with_group(int64_t dim, F&& f) {
         f(Int<V>{}, Int<1>{}, Int<64>{});
     else if (vecs <= 128)
         f(Int<V>{}, Int<2>{}, Int<64>{});
+    else if (vecs <= 192)
+        f(Int<V>{}, Int<3>{}, Int<64>{});
     else if (vecs <= 256)
         f(Int<V>{}, Int<1>{}, Int<256>{});
     else if (vecs <= 512)
