@@ -392,7 +392,7 @@ int scd_embed(const void *tokens_dev, int32_t token_type, int64_t n, const void 
  *   grad_dev: [n, dim];  out_dev: [rows, dim], of any element type.
  * The tokens are sorted first (a stable radix sort), so that each row is summed by its owner and written
  * once, without atomics.  scd_embed_grad_workspace gives the bytes of scratch that a call needs (16-byte
- * aligned, device). */
+ * aligned, device; 0 for short lists). */
 int scd_embed_grad_workspace(int64_t n, int64_t rows, int64_t dim, int64_t *bytes);
 int scd_embed_grad(const void *tokens_dev, int32_t token_type, int64_t n, const void *grad_dev, int32_t grad_type,
                    int64_t grad_stride, int64_t rows, int64_t dim, float scale, int32_t accumulate, void *out_dev,

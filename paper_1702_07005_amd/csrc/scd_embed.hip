@@ -643,6 +643,126 @@ __global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict
     }
 }
 
+// ---------------------------------------------------------------------------------------- few tokens
+// With at most kFewMax tokens one launch does it all: a workgroup owns some consecutive rows (and, of wide ones, a column
+// range), picks the tokens that lie in them, orders them by counting, fills the other rows with zeros and sums the runs,
+// long ones with several groups.  Every workgroup reads all tokens, so this is for lists that cost less than
+// the launches of a sort.
+constexpr int kFewMax = 1024;
+constexpr int kFewThreads = 1024;
+constexpr int kFewRows = 16384;  // of a workgroup at most: a bit each in LDS
+
+template <int VEC, bool ACC, typename TI, typename TG, typename TO>
+__global__ void __launch_bounds__(kFewThreads) k_grad_few(Tokens<TI> src, SumArgs a, const TG* __restrict__ grad, TO* __restrict__ out,
+                                                          uint32_t own_rows, uint32_t log2_lanes) {
+    constexpr int U = 8;
+    __shared__ uint32_t given[kFewRows / 32];    // the rows that have tokens
+    __shared__ __align__(16) uint32_t keys[kFewMax];
+    __shared__ uint32_t places[kFewMax];
+    __shared__ Pair sorted[kFewMax];
+    __shared__ uint32_t starts[kFewMax + 1], sums[kFewThreads / 64];
+    __shared__ float part[kFewThreads * VEC];
+    const uint32_t r0 = blockIdx.x * own_rows, here = min(own_rows, a.rows - r0), i = threadIdx.x;
+    const uint32_t m = kFewThreads >> log2_lanes, j = i >> log2_lanes, l = i & ((1u << log2_lanes) - 1);
+    const int32_t col = (int32_t)((blockIdx.y << log2_lanes) + l);
+    const bool in = col * VEC < a.dim;
+    int32_t again;
+    const int32_t c = vec_column<VEC>(in ? col : 0, a.dim, again);
+    for (uint32_t k = i; k < (here + 31) / 32; k += kFewThreads) given[k] = 0;
+    const uint32_t key = i < src.n ? src.key(i) - r0 : here;
+    const bool mine = key < here;  // also false for keys below r0, which wrap
+    uint32_t count, runs;
+    keys[i] = 0xFFFFFFFFu;  // above every key; block_exclusive waits for all
+    uint32_t at = block_exclusive(mine, sums, count);
+    if (mine) {
+        keys[at] = key;
+        places[at] = i;
+        atomicOr(&given[key / 32], 1u << key % 32);
+    }
+    __syncthreads();
+    if (i < count) {  // its place: how many of the keys before it in the list are at most its key, and of those after it less
+        const uint32_t own = keys[i], wave = i / 64;
+        uint32_t to = 0;
+        for (uint32_t b = 0; b * 64 < count; ++b) {
+            if (b != wave) {
+                const uint4* const q = reinterpret_cast<const uint4*>(keys + b * 64);
+                const uint32_t bound = own + (b < wave);
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) to += (q[k].x < bound) + (q[k].y < bound) + (q[k].z < bound) + (q[k].w < bound);
+            } else {
+                const uint32_t last = min(64u, count - b * 64);
+                for (uint32_t k = 0; k < last; ++k) to += keys[b * 64 + k] < own + (k < i % 64);
+            }
+        }
+        sorted[to] = Pair{own, places[i]};
+    }
+    __syncthreads();
+    const bool start = i < count && (i == 0 || sorted[i].key != sorted[i - 1].key);
+    at = block_exclusive(start, sums, runs);
+    if (start) starts[at] = i;
+    if (i == 0) starts[runs] = count;
+    __syncthreads();
+    if (!ACC && in) {
+        const float zero[VEC] = {};
+        for (uint32_t r = j; r < here; r += m)
+            if (!(given[r / 32] >> r % 32 & 1)) store_vec(out + (int64_t)(r0 + r) * a.ostride + c, zero);
+    }
+    const auto add = [&](uint32_t from, uint32_t end, uint32_t step, float (&s)[VEC]) {
+        for (uint32_t e = from; e < end; e += U * step) {
+            Raw<VEC, TG> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_raw<VEC>(grad + (int64_t)sorted[min(e + u * step, end - 1)].pos * a.gstride + c);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float x[VEC];
+                widen(v[u], x);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) s[k] += e + u * step < end ? x[k] : 0.0f;
+            }
+        }
+    };
+    constexpr uint32_t kLong = 2 * U;  // entries that a group sums alone
+    for (uint32_t q = j; q < runs && in; q += m) {
+        const uint32_t from = starts[q], end = starts[q + 1];
+        if (end - from > kLong && m > 1) continue;
+        float s[VEC] = {};
+        add(from, end, 1, s);
+        write_row<VEC, ACC>(a, out, r0 + sorted[from].key, c, again, s);
+    }
+    if (log2_lanes < 6) {  // a wave for each longer run
+        const uint32_t beside = 64 >> log2_lanes;
+        for (uint32_t q = i / 64; q < runs; q += kFewThreads / 64) {
+            const uint32_t from = starts[q], end = starts[q + 1];
+            if (end - from <= kLong) continue;
+            float s[VEC] = {};
+            if (in && from + j % beside < end) add(from + j % beside, end, beside, s);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                for (int o = 32; o >= 1 << log2_lanes; o /= 2) s[k] += __shfl_xor(s[k], o);
+            if (j % beside == 0 && in) write_row<VEC, ACC>(a, out, r0 + sorted[from].key, c, again, s);
+        }
+        return;
+    }
+    if (m == 1) return;
+    for (uint32_t q = 0; q < runs; ++q) {
+        const uint32_t from = starts[q], end = starts[q + 1];
+        if (end - from <= kLong) continue;
+        float s[VEC] = {};
+        if (in) add(from + j, end, m, s);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) part[i * VEC + k] = s[k];
+        __syncthreads();
+        if (j == 0 && in) {
+            const uint32_t parts = min(m, end - from);
+            for (uint32_t k = 1; k < parts; ++k)
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) s[v] += part[((k << log2_lanes) + l) * VEC + v];
+            write_row<VEC, ACC>(a, out, r0 + sorted[from].key, c, again, s);
+        }
+        __syncthreads();
+    }
+}
+
 // ---------------------------------------------------------------------------------------- host
 
 // Elements per thread and row: 16 bytes of the wider of the two types; 1 where a row has fewer.
@@ -667,6 +787,7 @@ bool is_token(int32_t t) { return t == SCD_I32 || t == SCD_I64; }
 
 // How a gradient call sorts and splits: a function of the sizes alone.
 struct Plan {
+    bool few;         // no sorted list: nothing below is used
     int64_t n;        // padded to whole batches
     bool tiled;       // a short list
     int passes, bits;
@@ -683,6 +804,8 @@ int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
 
 Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     Plan p{};
+    p.few = n <= kFewMax;
+    if (p.few) return p;
     p.n = ceil_div(n, kBatch) * kBatch;
     p.tiled = p.n <= kTiledMax;
     const int key_bits = std::max(1, (int)log2_up((uint64_t)rows + 1));
@@ -718,18 +841,15 @@ Fill fill_part(const Fill& f, int64_t part, int64_t parts) {
 template <typename TI>
 int sort_short(Tokens<TI> src, const Plan& p, Pair* pairs, Pair* other, const Fill& fill, hipStream_t s) {
     const uint32_t tiles = (uint32_t)ceil_div(p.n, kSmallTile), blocks = (uint32_t)ceil_div(p.n, 64);
-    const int launches = tiles > 1 ? 2 : 1;
-    Fill part = fill_part(fill, 0, launches);
-    k_sort_tiles<<<tiles + fill_blocks(part, 4 * kSmallTile), 4 * kSmallTile, 0, s>>>(src, (uint32_t)p.n, launches > 1 ? other : pairs, tiles, part);
-    if (launches > 1) {
-        const size_t lds = (size_t)(tiles * kSmallTile + kMergeThreads) * 4;
-        if (lds > 65536) {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_merge), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            if (e != hipSuccess) return fail(SCD_ERR_HIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-        }
-        part = fill_part(fill, 1, launches);
-        k_sort_merge<<<blocks + fill_blocks(part, kMergeThreads), kMergeThreads, lds, s>>>(other, (uint32_t)p.n, pairs, blocks, part);
+    Fill part = fill_part(fill, 0, 2);
+    k_sort_tiles<<<tiles + fill_blocks(part, 4 * kSmallTile), 4 * kSmallTile, 0, s>>>(src, (uint32_t)p.n, other, tiles, part);
+    const size_t lds = (size_t)(tiles * kSmallTile + kMergeThreads) * 4;
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_merge), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return fail(SCD_ERR_HIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
     }
+    part = fill_part(fill, 1, 2);
+    k_sort_merge<<<blocks + fill_blocks(part, kMergeThreads), kMergeThreads, lds, s>>>(other, (uint32_t)p.n, pairs, blocks, part);
     return launched("sort of tokens");
 }
 
@@ -803,11 +923,38 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
     if (!out || (n > 0 && (!tokens || !grad))) return fail(SCD_ERR_INVALID, "null device pointer");
     hipStream_t s = (hipStream_t)stream;
     const int64_t e = type_bytes(out_type);
+    const Plan p = plan_for(n, rows, dim);
+    if (p.bytes && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < p.bytes))
+        return fail(SCD_ERR_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)p.bytes);
+    SumArgs a{};
+    a.rows = (uint32_t)rows;
+    a.dim = (int32_t)dim;
+    a.scale = scale;
+    a.gstride = grad_stride;
+    a.ostride = rows > 1 ? out_stride : dim;
+    if (p.few) {
+        with_vec(grad_type, out_type, dim, [&](auto tg, auto to, auto vc) {
+            using TG = decltype(tg);
+            using TO = decltype(to);
+            constexpr int VEC = decltype(vc)::value;
+            const RowMap m = row_map(dim, VEC);
+            // A workgroup's rows: as many as let 512 workgroups, two to a CU, share the table, but 16 KB at least.
+            const int64_t least = ceil_div(16384, ((int64_t)VEC << m.log2_lanes) * (int64_t)sizeof(TO));
+            const int64_t own = std::min<int64_t>(kFewRows, std::max(least, ceil_div(rows * m.ranges, 512)));
+            const dim3 grid((uint32_t)ceil_div(rows, own), m.ranges);
+            const auto go = [&](auto ti, auto acc) {
+                using TI = decltype(ti);
+                k_grad_few<VEC, decltype(acc)::value><<<grid, kFewThreads, 0, s>>>(Tokens<TI>{(const TI*)tokens, n, (uint32_t)rows}, a, (const TG*)grad, (TO*)out, (uint32_t)own, m.log2_lanes);
+            };
+            if (token_type == SCD_I32)
+                accumulate ? go(int32_t{}, std::true_type{}) : go(int32_t{}, std::false_type{});
+            else
+                accumulate ? go(int64_t{}, std::true_type{}) : go(int64_t{}, std::false_type{});
+        });
+        return launched("scd_embed_grad");
+    }
     Fill fill{};
     if (!accumulate) fill = Fill{(char*)out, rows, dim * e, rows > 1 ? out_stride * e : dim * e};
-    const Plan p = plan_for(n, rows, dim);
-    if (n > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < p.bytes))
-        return fail(SCD_ERR_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)p.bytes);
     char* w = (char*)workspace;
     Pair* pairs = (Pair*)w;
     int rc = SCD_OK;
@@ -838,16 +985,10 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         sort(int32_t{});
     else
         sort(int64_t{});
-    if (rc != SCD_OK || n == 0) return rc;
-    SumArgs a{};
+    if (rc != SCD_OK) return rc;
     a.pairs = pairs;
     a.n = p.n;
     a.share = p.share;
-    a.rows = (uint32_t)rows;
-    a.dim = (int32_t)dim;
-    a.scale = scale;
-    a.gstride = grad_stride;
-    a.ostride = rows > 1 ? out_stride : dim;
     a.head = (float*)(w + 2 * p.pairs + p.hist);
     a.tail = (float*)((char*)a.head + p.pieces);
     with_vec(grad_type, out_type, dim, [&](auto tg, auto to, auto vc) {
@@ -865,7 +1006,7 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
                 k_sums_join<VEC, ACC, THREADS><<<blocks, THREADS, 0, s>>>(a, (TO*)out, m.log2_lanes);
             };
             // Wide rows get workgroups of several groups all the same.
-            if (p.groups > 1) m.log2_lanes >= 6 ? join(Int<1024>{}) : join(Int<kThreads>{});
+            m.log2_lanes >= 6 ? join(Int<1024>{}) : join(Int<kThreads>{});
         };
         accumulate ? go(std::true_type{}) : go(std::false_type{});
     });

@@ -152,9 +152,9 @@ def embed_grad(tokens, grad, rows, scale=1.0, out=None, accumulate=False, dtype=
         if dtype not in _TYPES:
             raise ValueError("dtype must be float32, bfloat16 or float16")
         out = torch.empty((rows, dim), dtype=dtype, device=device)
-    work = torch.empty(need, dtype=torch.uint8, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _check(lib.scd_embed_grad(tokens.data_ptr(), ids, n, grad.data_ptr(), kind, gstride, rows, dim, scale, bool(accumulate),
-                              out.data_ptr(), _TYPES[dtype], ostride, work.data_ptr(), need, _current_stream(device.index)))
+                              out.data_ptr(), _TYPES[dtype], ostride, work.data_ptr() if need else None, need, _current_stream(device.index)))
     return out
 
 

@@ -88,9 +88,9 @@ def test_embed_grad_refusals(lib):
     for kw in (dict(tok=None), dict(grad=None), dict(out=None)):
         _refused(lib, -1, "null device pointer", call(**kw))
     need = ctypes.c_int64()
-    assert lib.scd_embed_grad_workspace(4, 10, 8, ctypes.byref(need)) == 0 and need.value > 0
+    assert lib.scd_embed_grad_workspace(4000, 10, 8, ctypes.byref(need)) == 0 and need.value > 0
     for kw in (dict(work=None), dict(work=P + 8), dict(wb=need.value - 1)):
-        _refused(lib, -1, "workspace", call(**kw))
+        _refused(lib, -1, "workspace", call(n=4000, **kw))
     assert call(rows=0, out=None) == 0
     assert call(n=0, acc=1, tok=None, grad=None, work=None) == 0
     _refused(lib, -1, "bad sizes", lib.scd_embed_grad_workspace(4, 10, 0, ctypes.byref(need)))

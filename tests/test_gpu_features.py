@@ -481,3 +481,30 @@ def test_refusals():
               lambda: features.clip_grads([x], -1.0), lambda: features.embed_grad(ids, x, -1)):
         with pytest.raises(scd.ScdError):
             f()
+
+
+# Few tokens take one launch without a sort; around its limit of 512, with long runs, wide rows and more rows than one
+# workgroup's 16,384.
+@pytest.mark.parametrize("kind", ["even", "zipf", "one", "none", "outside"])
+@pytest.mark.parametrize("n,rows,dim", [(2, 40_000, 3), (64, 20, 40), (300, 17_000_000, 1), (511, 33, 2050), (512, 700, 130), (513, 700, 130)])
+def test_embed_grad_few_tokens(kind, n, rows, dim):
+    g = _gen(n + rows + dim)
+    t = _tokens(g, n, rows, kind)
+    d = _normal(g, n, dim, dtype=torch.bfloat16)
+    got = features.embed_grad(t.to(DEV), d.to(DEV), rows, dtype=torch.float32)
+    want = fo.embed_grad(t, d, rows, 1.0, torch.float32)
+    fo.close(got, want, f"embed_grad {kind}")
+    got.fill_(0.5)
+    features.embed_grad(t.to(DEV), d.to(DEV), rows, out=got, accumulate=True)
+    if rows < 1_000_000:
+        fo.close(got, fo.embed_grad(t, d, rows, 1.0, torch.float32, torch.full((rows, dim), 0.5)), f"embed_grad {kind}")
+
+
+@pytest.mark.parametrize("kind", ["zipf", "one", "outside"])
+@pytest.mark.parametrize("n,rows,dim", [(1023, 90, 17), (1024, 2, 260), (1024, 5000, 64), (1025, 5000, 64), (700, 64, 3)])
+def test_embed_grad_few_tokens_long_runs(kind, n, rows, dim):
+    g = _gen(n + rows + dim)
+    t = _tokens(g, n, rows, kind)
+    d = _normal(g, n, dim)
+    got = features.embed_grad(t.to(DEV), d.to(DEV), rows)
+    fo.close(got, fo.embed_grad(t, d, rows, 1.0, torch.float32), f"embed_grad {kind}")
