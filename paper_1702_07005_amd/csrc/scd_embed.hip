@@ -36,7 +36,12 @@ RowMap row_map(int64_t dim, int vec) {
 
 // ---------------------------------------------------------------------------------------- lookup
 
-template <int VEC, int U, typename TI, typename TT, typename TO>
+// A large output goes past the caches (ONCE), so that the table's rows stay there.  2.6 M ids into 1.5 M x 16 (fp32, 164 MB
+// out): 63 us through the caches, 53 past them; 16,384 x 4,096 (bf16, 134 MB): 42 and 34, and with the layer norm that
+// reads them 88 and 86; but 4,096 x 4,096 (34 MB), which the norm then finds in the caches: 22.8 and 25.7 together.
+constexpr int64_t kOnceBytes = int64_t(96) << 20;
+
+template <int VEC, int U, bool ONCE, typename TI, typename TT, typename TO>
 __global__ void __launch_bounds__(kThreads) k_embed(const TI* __restrict__ tok, int64_t n, const TT* __restrict__ table,
                                                     int64_t tstride, int64_t rows, int32_t dim, float scale,
                                                     TO* __restrict__ out, int64_t ostride, uint32_t log2_lanes) {
@@ -62,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) k_embed(const TI* __restrict__ tok, 
         const float other = id[u] < 0 ? 0.0f : __builtin_nanf("");
 #pragma unroll
         for (int i = 0; i < VEC; ++i) o[i] = in ? scale * o[i] : other;
-        if (g + u * groups < n) store_vec(out + (g + u * groups) * ostride + c, o);
+        if (g + u * groups < n) put_vec<ONCE>(out + (g + u * groups) * ostride + c, o);
     }
 }
 
@@ -112,8 +117,9 @@ __device__ __forceinline__ void fill_bytes(char* p, int64_t bytes, int64_t worke
 }
 
 __device__ __forceinline__ void fill_zero(const Fill& f, uint32_t block, uint32_t blocks) {
-    if (f.stride == f.row_bytes) {
-        fill_bytes(f.p, f.rows * f.row_bytes, (int64_t)block * blockDim.x + threadIdx.x, (int64_t)blocks * blockDim.x);
+    if (f.stride == f.row_bytes) {  // a run of whole 64-byte lines for each workgroup
+        const int64_t total = f.rows * f.row_bytes, share = (total / blocks + 63) / 64 * 64, from = min(total, block * share);
+        fill_bytes(f.p + from, min(share, total - from), threadIdx.x, blockDim.x);
         return;
     }
     const int64_t waves = (int64_t)blocks * (blockDim.x / 64);
@@ -123,13 +129,15 @@ __device__ __forceinline__ void fill_zero(const Fill& f, uint32_t block, uint32_
 
 // The lanes of the wave that hold the same digit as this one, among the active ones.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits) {
-    uint64_t m = __ballot(1);
+    const uint64_t all = __ballot(1);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
     for (int b = 0; b < bits; ++b) {
-        const bool on = (digit >> b) & 1;
-        const uint64_t v = __ballot(on);
-        m &= on ? v : ~v;
+        const uint32_t mine = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);  // all ones where the bit is set
+        const uint64_t set = __ballot(mine != 0);
+        lo &= ~((uint32_t)set ^ mine);
+        hi &= ~((uint32_t)(set >> 32) ^ mine);
     }
-    return m;
+    return (uint64_t)hi << 32 | lo;
 }
 
 __device__ __forceinline__ uint32_t lanes_below(uint64_t m) {
@@ -162,7 +170,7 @@ __device__ __forceinline__ uint32_t block_exclusive(uint32_t x, uint32_t* wave_s
 // zeroed) becomes the wave's number of keys with that digit.
 template <int J>
 __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[J], const bool (&on)[J], int bits,
-                                           volatile uint16_t* counts, uint32_t (&rank)[J]) {
+                                           uint16_t* counts, uint32_t (&rank)[J]) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         if (!on[j]) continue;
@@ -170,9 +178,9 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[J], const boo
         const uint32_t below = lanes_below(m);
         const uint32_t base = counts[digit[j]];
         rank[j] = base + below;
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // LDS serves a wave's accesses in order
         if (below == 0) counts[digit[j]] = (uint16_t)(base + (uint32_t)__popcll(m));
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -262,18 +270,16 @@ __global__ void __launch_bounds__(kMergeThreads) k_sort_merge(const Pair* __rest
     }
 }
 
-// Long lists: a radix sort from the lowest digit up, a workgroup for each tile of kTile consecutive entries.  A pass
+// Long lists: a radix sort from the lowest digit up, a workgroup for each tile of kTileThreads x J consecutive entries.  A pass
 // counts the tiles' digits (k_sort_count), sums the counts along the tiles (k_sort_scan), and moves the entries
 // (k_sort_move), which orders its tile in LDS first, so that it writes runs of consecutive entries.  Every launch
 // fills a part of the zeros with further workgroups.
 constexpr int kTileThreads = 512;
-constexpr int kTileJ = 8;
-constexpr int kTile = kTileThreads * kTileJ;
 constexpr int kTileWaves = kTileThreads / 64;
 constexpr int kMaxBits = 11;
 constexpr int kPer = (1 << kMaxBits) / kTileThreads;  // digits a thread at most: k_sort_move gives it consecutive ones
 
-template <typename SRC>
+template <int J, typename SRC>
 __global__ void __launch_bounds__(kTileThreads) k_sort_count(SRC src, int64_t n, int shift, int bits, uint32_t tiles,
                                                              uint32_t* __restrict__ hist, Fill fill) {
     if (blockIdx.x >= tiles) {
@@ -284,9 +290,9 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_count(SRC src, int64_t n,
     const uint32_t bins = 1u << bits;
     for (uint32_t d = threadIdx.x; d < bins; d += kTileThreads) count[d] = 0;
     __syncthreads();
-    const int64_t base = (int64_t)blockIdx.x * kTile;
+    const int64_t base = (int64_t)blockIdx.x * (kTileThreads * J);
 #pragma unroll
-    for (int j = 0; j < kTileJ; ++j) {
+    for (int j = 0; j < J; ++j) {
         const int64_t i = base + j * kTileThreads + threadIdx.x;
         if (i < n) atomicAdd(&count[(src.key(i) >> shift) & (bins - 1)], 1u);
     }
@@ -341,7 +347,7 @@ __global__ void __launch_bounds__(kScanDigits * kScanSlices) k_sort_scan(uint32_
     if (on && slice == 0) totals[d] = total;
 }
 
-template <typename SRC>
+template <int J, typename SRC>
 __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, int shift, int bits, uint32_t tiles,
                                                             const uint32_t* __restrict__ hist,
                                                             const uint32_t* __restrict__ totals, Pair* __restrict__ out, Fill fill) {
@@ -349,6 +355,7 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
         fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
         return;
     }
+    constexpr int kTile = kTileThreads * J;
     __shared__ Pair tile[kTile];
     extern __shared__ __align__(16) uint32_t shift_of[];              // [digit]: from a place in the ordered tile to that in `out`
     uint16_t* const counts = reinterpret_cast<uint16_t*>(shift_of + (1 << bits));  // [wave][digit]
@@ -356,12 +363,12 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
     const uint32_t bins = 1u << bits, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t per = max(1u, bins / kTileThreads), d0 = threadIdx.x * per;
     for (uint32_t i = threadIdx.x; i < kTileWaves * bins / 2; i += kTileThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
-    const int64_t base = (int64_t)blockIdx.x * kTile, at = base + wave * 64 * kTileJ + lane;
-    Pair p[kTileJ];
-    uint32_t digit[kTileJ], rank[kTileJ], all = 0, total;
-    bool on[kTileJ];
+    const int64_t base = (int64_t)blockIdx.x * kTile, at = base + wave * 64 * J + lane;
+    Pair p[J];
+    uint32_t digit[J], rank[J], all = 0, total;
+    bool on[J];
 #pragma unroll
-    for (int j = 0; j < kTileJ; ++j) {
+    for (int j = 0; j < J; ++j) {
         const int64_t i = at + j * 64;
         on[j] = i < n;
         p[j] = src.pair(on[j] ? i : 0);
@@ -377,7 +384,7 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
         all += t[k];
     }
     uint32_t start = block_exclusive(all, sums, total);
-    wave_ranks<kTileJ>(digit, on, bits, counts + wave * bins, rank);
+    wave_ranks<J>(digit, on, bits, counts + wave * bins, rank);
     __syncthreads();
     uint32_t here[kPer], sum = 0;
 #pragma unroll
@@ -405,12 +412,12 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
         }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kTileJ; ++j)
+    for (int j = 0; j < J; ++j)
         if (on[j]) tile[counts[wave * bins + digit[j]] + rank[j]] = p[j];
     __syncthreads();
     const uint32_t entries = (uint32_t)min((int64_t)kTile, n - base);
 #pragma unroll
-    for (int j = 0; j < kTileJ; ++j) {
+    for (int j = 0; j < J; ++j) {
         const uint32_t i = j * kTileThreads + threadIdx.x;
         if (i < entries) {
             const Pair q = tile[i];
@@ -476,7 +483,7 @@ __global__ void __launch_bounds__(kThreads) k_sums(SumArgs a, const TG* __restri
         Raw<VEC, TG> v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            v[u] = load_raw<VEC>(grad + (int64_t)p.t[u].pos * a.gstride + c);
+            v[u] = load_raw_once<VEC>(grad + (int64_t)p.t[u].pos * a.gstride + c);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p.t[u].key != cur) {
@@ -791,6 +798,7 @@ struct Plan {
     int64_t n;        // padded to whole batches
     bool tiled;       // a short list
     int passes, bits;
+    int per_thread;
     int64_t tiles;
     uint32_t share;
     int64_t groups;
@@ -798,6 +806,9 @@ struct Plan {
     int64_t hist, pieces, bytes;
 };
 
+// Lists of up to this many entries are sorted by tiles, or up to twice as many where the radix sort takes several passes.
+// Whole calls: 16,384 tokens into 1,000 x 256 (one pass) 28 us by tiles and 35 by radix, 30,000 46 and 38;
+// 30,000 into 300,000 x 64 (two passes) 47 and 58, 16,384 into 75,000 x 1,024 46 and 71.
 constexpr int64_t kTiledMax = 16384;
 
 int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
@@ -807,12 +818,16 @@ Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     p.few = n <= kFewMax;
     if (p.few) return p;
     p.n = ceil_div(n, kBatch) * kBatch;
-    p.tiled = p.n <= kTiledMax;
     const int key_bits = std::max(1, (int)log2_up((uint64_t)rows + 1));
     // Digits of 9 bits, or of up to 11 where that saves a pass: the more digits, the shorter the runs that a tile writes.
     p.passes = std::min((key_bits + 8) / 9, (key_bits + kMaxBits - 1) / kMaxBits);
+    p.tiled = p.n <= kTiledMax * (p.passes > 1 ? 2 : 1);
     p.bits = (key_bits + p.passes - 1) / p.passes;
-    p.tiles = ceil_div(p.n, kTile);
+    // Entries of a tile's thread: enough tiles for the CUs while the list is short, few counts of digits where it is long.
+    // Whole calls with 2, 4 and 8: 131,072 into 50,000 x 512 74, 77 and 84 us; 300,000 into 1.5 M x 32 78, 76 and 84;
+    // 600,000 into 1.5 M x 16 96, 89 and 90; 1.28 M into 1.5 M x 16 (4 and 8) 135 and 120.
+    p.per_thread = p.n <= 200'000 ? 2 : p.n <= 800'000 ? 4 : 8;
+    p.tiles = ceil_div(p.n, kTileThreads * p.per_thread);
     // Entries per group: as many as keep about 4,096 waves in work, 8 at least, 64 at most.
     const int64_t work = p.n * ceil_div(dim, 4) / 64;
     p.share = (uint32_t)std::min<int64_t>(64, std::max<int64_t>(8, work / 4096 / 8 * 8));
@@ -824,11 +839,11 @@ Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     return p;
 }
 
-// Workgroups of `threads` threads that fill a part of the zeros beside other work: 64 bytes a thread, up to eight waves
-// for each of the GPU's SIMDs.
+// Workgroups of `threads` threads that fill a part of the zeros beside other work: 64 bytes a thread, but at most 2 M
+// threads in all.
 uint32_t fill_blocks(const Fill& f, int threads) {
     if (!f.p) return 0;
-    return (uint32_t)std::min<int64_t>(ceil_div(f.rows * f.row_bytes, threads * 64), 512 * (1024 / threads));
+    return (uint32_t)std::min<int64_t>(ceil_div(f.rows * f.row_bytes, threads * 64), 2048 * (1024 / threads));
 }
 
 // The first `part` of `parts` equal parts, the second, ...
@@ -853,13 +868,13 @@ int sort_short(Tokens<TI> src, const Plan& p, Pair* pairs, Pair* other, const Fi
     return launched("sort of tokens");
 }
 
-template <typename SRC>
+template <int J, typename SRC>
 void launch_pass(SRC src, int pass, const Plan& p, uint32_t* hist, uint32_t* totals, Pair* out, const Fill* fills, hipStream_t s) {
     const uint32_t tiles = (uint32_t)p.tiles, scans = (uint32_t)ceil_div(1 << p.bits, kScanDigits);
     const int shift = pass * p.bits;
-    k_sort_count<<<tiles + fill_blocks(fills[0], kTileThreads), kTileThreads, 0, s>>>(src, p.n, shift, p.bits, tiles, hist, fills[0]);
+    k_sort_count<J><<<tiles + fill_blocks(fills[0], kTileThreads), kTileThreads, 0, s>>>(src, p.n, shift, p.bits, tiles, hist, fills[0]);
     k_sort_scan<<<scans + fill_blocks(fills[1], kScanDigits * kScanSlices), kScanDigits * kScanSlices, 0, s>>>(hist, tiles, p.bits, totals, scans, fills[1]);
-    k_sort_move<<<tiles + fill_blocks(fills[2], kTileThreads), kTileThreads, (4 + 2 * kTileWaves) << p.bits, s>>>(src, p.n, shift, p.bits, tiles, hist, totals, out, fills[2]);
+    k_sort_move<J><<<tiles + fill_blocks(fills[2], kTileThreads), kTileThreads, (4 + 2 * kTileWaves) << p.bits, s>>>(src, p.n, shift, p.bits, tiles, hist, totals, out, fills[2]);
 }
 
 }  // namespace
@@ -888,16 +903,21 @@ extern "C" int scd_embed(const void* tokens, int32_t token_type, int64_t n, cons
         using TT = decltype(tt);
         using TO = decltype(to);
         constexpr int VEC = decltype(vc)::value;
-        const auto go = [&](auto ti, auto uc) {
+        const auto go = [&](auto ti, auto uc, auto once) {
             using TI = decltype(ti);
             constexpr int U = decltype(uc)::value;
-            k_embed<VEC, U><<<grid, kThreads, 0, (hipStream_t)stream>>>((const TI*)tokens, n, (const TT*)table, table_stride, rows,
-                                                                       (int32_t)dim, scale, (TO*)out, out_stride, m.log2_lanes);
+            k_embed<VEC, U, decltype(once)::value><<<grid, kThreads, 0, (hipStream_t)stream>>>((const TI*)tokens, n, (const TT*)table, table_stride, rows,
+                                                                                             (int32_t)dim, scale, (TO*)out, out_stride, m.log2_lanes);
         };
-        if (token_type == SCD_I32)
-            U == 4 ? go(int32_t{}, Int<4>{}) : go(int32_t{}, Int<1>{});
-        else
-            U == 4 ? go(int64_t{}, Int<4>{}) : go(int64_t{}, Int<1>{});
+        const auto with_ids = [&](auto ti) {
+            if (U == 1)
+                go(ti, Int<1>{}, std::false_type{});
+            else if (n * dim * type_bytes(out_type) < kOnceBytes)
+                go(ti, Int<4>{}, std::false_type{});
+            else
+                go(ti, Int<4>{}, std::true_type{});
+        };
+        token_type == SCD_I32 ? with_ids(int32_t{}) : with_ids(int64_t{});
     });
     return launched("scd_embed");
 }
@@ -973,10 +993,14 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         for (int k = 0; k < p.passes; ++k) {
             const Fill part[3] = {fill_part(fill, 3 * k, launches), fill_part(fill, 3 * k + 1, launches), fill_part(fill, 3 * k + 2, launches)};
             Pair* const to = k % 2 ? other : pairs;
-            if (k == 0)
-                launch_pass(src, k, p, hist, totals, to, part, s);
-            else
-                launch_pass(Pairs{k % 2 ? pairs : other}, k, p, hist, totals, to, part, s);
+            const auto pass = [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if (k == 0)
+                    launch_pass<J>(src, k, p, hist, totals, to, part, s);
+                else
+                    launch_pass<J>(Pairs{k % 2 ? pairs : other}, k, p, hist, totals, to, part, s);
+            };
+            p.per_thread == 2 ? pass(Int<2>{}) : p.per_thread == 4 ? pass(Int<4>{}) : pass(Int<8>{});
         }
         if (p.passes % 2 == 0) pairs = other;
         rc = launched("sort of tokens");

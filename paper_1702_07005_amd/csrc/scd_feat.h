@@ -52,6 +52,52 @@ __device__ __forceinline__ void store_vec(T* __restrict__ p, const float (&v)[N]
     __builtin_memcpy(p, &r, sizeof r);
 }
 
+// The same past the caches (non-temporal): for data that is touched once and larger than what the caches would keep.
+template <int BYTES>
+struct Words {
+    typedef uint32_t type __attribute__((ext_vector_type(BYTES / 4), aligned(2)));
+};
+template <>
+struct Words<2> {
+    typedef uint16_t type;
+};
+template <>
+struct Words<4> {
+    typedef uint32_t type __attribute__((aligned(2)));
+};
+
+template <int N, typename T>
+__device__ __forceinline__ Raw<N, T> load_raw_once(const T* __restrict__ p) {
+    using W = typename Words<sizeof(Raw<N, T>)>::type;
+    const W w = __builtin_nontemporal_load(reinterpret_cast<const W*>(p));
+    return __builtin_bit_cast(Raw<N, T>, w);
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_vec_once(T* __restrict__ p, const float (&v)[N]) {
+    using W = typename Words<sizeof(Raw<N, T>)>::type;
+    Raw<N, T> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.t[i] = (T)v[i];
+    __builtin_nontemporal_store(__builtin_bit_cast(W, r), reinterpret_cast<W*>(p));
+}
+
+template <int N, bool ONCE, typename T>
+__device__ __forceinline__ Raw<N, T> fetch_raw(const T* __restrict__ p) {
+    if constexpr (ONCE)
+        return load_raw_once<N>(p);
+    else
+        return load_raw<N>(p);
+}
+
+template <bool ONCE, int N, typename T>
+__device__ __forceinline__ void put_vec(T* __restrict__ p, const float (&v)[N]) {
+    if constexpr (ONCE)
+        store_vec_once(p, v);
+    else
+        store_vec(p, v);
+}
+
 // Vectors of a row: the k-th begins at column k N, except the last of a width that N does not divide, which
 // begins at dim - N instead and repeats `again` columns of the one before it.  Every vector is whole (dim >= N),
 // so there is no code for tails; what is computed per column comes out the same in both, and sums over

@@ -199,7 +199,12 @@ struct NormGradArgs {
     float* sums;  // [workgroups][2][dim] of dw and db, or null
 };
 
-template <int VEC, int NV, int LPR, int THREADS, typename T, typename P>
+// Where the three matrices take more than the caches hold (ONCE), they are read and written past them: 50,000 x 624
+// (fp32, 374 MB) 71.8 us through the caches, 66.3 past them, 16,384 x 4,096 (bf16, 403 MB) 79.5 and 76.5; but
+// 4,096 x 4,096 (101 MB), whose inputs the caches may hold, 24.8 and 30.4.
+constexpr int64_t kOnceBytes = int64_t(288) << 20;
+
+template <int VEC, int NV, int LPR, int THREADS, bool ONCE, typename T, typename P>
 __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
     constexpr int kGroups = THREADS / LPR;
     constexpr int kElems = LPR * NV * VEC;
@@ -217,9 +222,9 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
     const auto fetch = [&](int64_t row) {
         row = min(row, (int64_t)a.rows - 1);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) ndy[j] = load_raw<VEC>(a.dy + row * a.gstride + col.at[j]);
+        for (int j = 0; j < NV; ++j) ndy[j] = fetch_raw<VEC, ONCE>(a.dy + row * a.gstride + col.at[j]);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) nx[j] = load_raw<VEC>(a.x + row * a.xstride + col.at[j]);
+        for (int j = 0; j < NV; ++j) nx[j] = fetch_raw<VEC, ONCE>(a.x + row * a.xstride + col.at[j]);
         nmean = a.mean[row];
         nrstd = a.rstd[row];
     };
@@ -267,7 +272,7 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
             for (int j = 0; j < NV; ++j) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) dy[j][i] = rstd * (dy[j][i] - c1 - h[j][i] * c2);
-                if (col.skip[j] < VEC) store_vec(a.dx + r * a.dstride + col.at[j], dy[j]);
+                if (col.skip[j] < VEC) put_vec<ONCE>(a.dx + r * a.dstride + col.at[j], dy[j]);
             }
         }
     }
@@ -358,8 +363,9 @@ __global__ void __launch_bounds__(64 * kSlices) k_norm_params(const float* __res
 // ---------------------------------------------------------------------------------------- host
 
 // Calls f(Int<VEC>, Int<NV>, Int<LPR>) with the smallest group that holds a row of `dim` elements of T, or returns
-// false where none does.
-template <typename T, typename F>
+// false where none does.  A wave holds four vectors a lane, but in the backward pass, which keeps six values per element,
+// of 16-bit elements three.
+template <typename T, bool GRAD, typename F>
 bool with_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
     const int64_t vecs = ceil_div(dim, V);
@@ -380,7 +386,7 @@ bool with_group(int64_t dim, F&& f) {
     else if (vecs <= 192)
         f(Int<V>{}, Int<3>{}, Int<64>{});
     else if (vecs <= 256)
-        f(Int<V>{}, Int<1>{}, Int<256>{});
+        f(Int<V>{}, Int<GRAD && V == 8 ? 1 : 4>{}, Int<GRAD && V == 8 ? 256 : 64>{});
     else if (vecs <= 512)
         f(Int<V>{}, Int<2>{}, Int<256>{});
     else if (vecs <= 1024)
@@ -437,7 +443,7 @@ extern "C" int scd_layer_norm(const void* x, int32_t type, int64_t x_stride, int
         using T = decltype(t);
         using P = decltype(p);
         const NormArgs<T, P> a{(const T*)x, x_stride, (int32_t)rows, (int32_t)dim, (const P*)weight, (const P*)bias, eps, (T*)y, y_stride, mean, rstd};
-        const bool fits = with_group<T>(dim, [&](auto vec, auto nv, auto lpr) {
+        const bool fits = with_group<T, false>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
             const int64_t blocks = std::min<int64_t>(kBlocks, ceil_div(rows, THREADS / LPR));
@@ -477,11 +483,14 @@ extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const 
         const NormGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)x, x_stride, mean, rstd, (int32_t)rows, (int32_t)dim, (const P*)weight, (T*)dx, dx_stride, sums};
         int64_t blocks = grad_blocks(rows);
         if (rows > 0) {
-            const bool fits = with_group<T>(dim, [&](auto vec, auto nv, auto lpr) {
+            const bool fits = with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
                 constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
                 constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
                 blocks = std::min<int64_t>(blocks, ceil_div(rows, THREADS / LPR));
-                k_norm_grad<VEC, NV, LPR, THREADS><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+                if (rows * dim * 3 * (int64_t)sizeof(T) < kOnceBytes)
+                    k_norm_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+                else
+                    k_norm_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
             });
             if (!fits) k_norm_grad_wide<<<(uint32_t)blocks, kWideThreads, 0, s>>>(a);
         }
