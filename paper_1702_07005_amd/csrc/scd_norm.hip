@@ -77,7 +77,11 @@ struct NormArgs {
     float* rstd;
 };
 
-template <int VEC, int NV, int LPR, int THREADS, typename T, typename P>
+// A large output goes past the caches (ONCE): 100,000 x 624 (fp32, 250 MB out) 98.4 us through them, 95.5 past them,
+// 16,384 x 2,048 (bf16, 67 MB) 25.3 and 22.4; a smaller one is left there for its reader.
+constexpr int64_t kOnceOut = int64_t(64) << 20;
+
+template <int VEC, int NV, int LPR, int THREADS, bool ONCE, typename T, typename P>
 __global__ void __launch_bounds__(THREADS) k_norm(NormArgs<T, P> a) {
     __shared__ float lds[lds_words<LPR, THREADS>(2)];
     constexpr int kGroups = THREADS / LPR;
@@ -139,7 +143,7 @@ __global__ void __launch_bounds__(THREADS) k_norm(NormArgs<T, P> a) {
                 widen(b[j], bj);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) y[i] = x[j][i] * rstd * wj[i] + bj[i];
-                if (col.skip[j] < VEC) store_vec(a.y + r * a.ystride + col.at[j], y);
+                if (col.skip[j] < VEC) put_vec<ONCE>(a.y + r * a.ystride + col.at[j], y);
             }
             if (lane == 0) {
                 if (a.mean) a.mean[r] = mean;
@@ -197,6 +201,8 @@ struct NormGradArgs {
     T* dx;
     int64_t dstride;
     float* sums;  // [workgroups][2][dim] of dw and db, or null
+    P* dw;        // not null with one workgroup: its sums are the results
+    P* db;
 };
 
 // Where the three matrices take more than the caches hold (ONCE), they are read and written past them: 50,000 x 624
@@ -276,9 +282,10 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
             }
         }
     }
-    if (!a.sums) return;
-    float* const out = a.sums + (int64_t)blockIdx.x * 2 * a.dim;
+    if (!a.sums && !a.dw) return;
+    float* const sums = a.sums + (int64_t)blockIdx.x * 2 * a.dim;
     for (int which = 0; which < 2; ++which) {
+        P* const result = which ? a.db : a.dw;
         if constexpr (kGroups > 1) {
             __syncthreads();
 #pragma unroll
@@ -294,12 +301,20 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
                 float s = 0.0f;
 #pragma unroll
                 for (int k = 0; k < kGroups; ++k) s += part[k * kElems + e];
-                out[which * a.dim + c] = s;
+                if (a.dw)
+                    result[c] = (P)s;
+                else
+                    sums[which * a.dim + c] = s;
             }
         } else {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                if (col.skip[j] < VEC) store_vec(out + which * a.dim + col.at[j], which ? db[j] : dw[j]);
+                if (col.skip[j] < VEC) {
+                    if (a.dw)
+                        store_vec(result + col.at[j], which ? db[j] : dw[j]);
+                    else
+                        store_vec(sums + which * a.dim + col.at[j], which ? db[j] : dw[j]);
+                }
         }
     }
 }
@@ -309,6 +324,17 @@ __global__ void __launch_bounds__(kWideThreads) k_norm_grad_wide(NormGradArgs<T,
     __shared__ float lds[lds_words<kWideThreads, kWideThreads>(2)];
     const float inv = 1.0f / (float)a.dim;
     float* const dw = a.sums ? a.sums + (int64_t)blockIdx.x * 2 * a.dim : nullptr;
+    if (a.dw)  // before dx, which may lie in x's or dy's place; each thread its own columns, here and below
+        for (int32_t c = threadIdx.x; c < a.dim; c += kWideThreads) {
+            float sw = 0.0f, sb = 0.0f;
+            for (int64_t r = 0; r < a.rows; ++r) {
+                const float d = (float)a.dy[r * a.gstride + c];
+                sw += d * (((float)a.x[r * a.xstride + c] - a.mean[r]) * a.rstd[r]);
+                sb += d;
+            }
+            a.dw[c] = (P)sw;
+            a.db[c] = (P)sb;
+        }
     int turn = 0;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
         const T* const dy = a.dy + r * a.gstride;
@@ -320,7 +346,7 @@ __global__ void __launch_bounds__(kWideThreads) k_norm_grad_wide(NormGradArgs<T,
             const float d = (float)dy[c], h = ((float)x[c] - mean) * rstd, g = d * (a.weight ? (float)a.weight[c] : 1.0f);
             s[0] += g;
             s[1] += g * h;
-            if (dw) {  // each thread its own columns
+            if (a.sums) {  // each thread its own columns
                 const bool first = r == blockIdx.x;
                 dw[c] = (first ? 0.0f : dw[c]) + d * h;
                 dw[a.dim + c] = (first ? 0.0f : dw[a.dim + c]) + d;
@@ -423,6 +449,12 @@ int check_norm(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {
 
 int64_t grad_blocks(int64_t rows) { return std::min<int64_t>(rows, kGradBlocks); }
 
+// Up to this many rows for each group of a workgroup, one workgroup does it all, which saves the second launch; a call of
+// so few rows needs no workspace, whatever its groups.
+constexpr int64_t kTurnsAlone = 2;
+
+int64_t grad_workspace(int64_t rows, int64_t dim) { return rows <= kTurnsAlone ? 0 : grad_blocks(rows) * 2 * dim * 4; }
+
 }  // namespace
 }  // namespace feat
 }  // namespace scd
@@ -447,7 +479,10 @@ extern "C" int scd_layer_norm(const void* x, int32_t type, int64_t x_stride, int
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
             const int64_t blocks = std::min<int64_t>(kBlocks, ceil_div(rows, THREADS / LPR));
-            k_norm<VEC, NV, LPR, THREADS><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+            if (rows * dim * (int64_t)sizeof(T) < kOnceOut)
+                k_norm<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+            else
+                k_norm<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
         });
         if (!fits) k_norm_wide<<<(uint32_t)std::min<int64_t>(kBlocks, rows), kWideThreads, 0, s>>>(a);
     });
@@ -458,7 +493,7 @@ extern "C" int scd_layer_norm_grad_workspace(int64_t rows, int64_t dim, int64_t*
     if (!bytes) return fail(SCD_ERR_INVALID, "bytes is null");
     *bytes = 0;
     if (int r = check_norm(SCD_F32, SCD_F32, rows, dim)) return r;
-    *bytes = grad_blocks(rows) * 2 * dim * 4;
+    *bytes = grad_workspace(rows, dim);
     return SCD_OK;
 }
 
@@ -472,29 +507,36 @@ extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const 
         return fail(SCD_ERR_INVALID, "in place the strides must be the same");
     if (!dweight != !dbias) return fail(SCD_ERR_INVALID, "dweight and dbias go together");
     if (rows > 0 && (!grad || !x || !mean || !rstd || !dx)) return fail(SCD_ERR_INVALID, "null device pointer");
-    const int64_t need = dweight ? grad_blocks(rows) * 2 * dim * 4 : 0;
+    const int64_t need = dweight ? grad_workspace(rows, dim) : 0;
     if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need))
         return fail(SCD_ERR_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)need);
     hipStream_t s = (hipStream_t)stream;
     with_types(type, param_type, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        float* const sums = dweight ? (float*)workspace : nullptr;
-        const NormGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)x, x_stride, mean, rstd, (int32_t)rows, (int32_t)dim, (const P*)weight, (T*)dx, dx_stride, sums};
-        int64_t blocks = grad_blocks(rows);
-        if (rows > 0) {
-            const bool fits = with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
-                constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
-                constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
-                blocks = std::min<int64_t>(blocks, ceil_div(rows, THREADS / LPR));
-                if (rows * dim * 3 * (int64_t)sizeof(T) < kOnceBytes)
-                    k_norm_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
-                else
-                    k_norm_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
-            });
-            if (!fits) k_norm_grad_wide<<<(uint32_t)blocks, kWideThreads, 0, s>>>(a);
+        NormGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)x, x_stride, mean, rstd, (int32_t)rows, (int32_t)dim, (const P*)weight, (T*)dx, dx_stride, nullptr, nullptr, nullptr};
+        int64_t blocks = 0;
+        const auto share = [&](int64_t groups) {  // the workgroups, and where their sums go
+            const bool alone = rows <= kTurnsAlone * groups;
+            blocks = alone && dweight ? 1 : std::min<int64_t>(kGradBlocks, ceil_div(rows, groups));
+            a.dw = alone ? (P*)dweight : nullptr;
+            a.db = alone ? (P*)dbias : nullptr;
+            a.sums = alone || !dweight ? nullptr : (float*)workspace;
+        };
+        const bool fits = rows > 0 && with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
+            constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
+            constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
+            share(THREADS / LPR);
+            if (rows * dim * 3 * (int64_t)sizeof(T) < kOnceBytes)
+                k_norm_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+            else
+                k_norm_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+        });
+        if (rows > 0 && !fits) {
+            share(1);
+            k_norm_grad_wide<<<(uint32_t)blocks, kWideThreads, 0, s>>>(a);
         }
-        if (dweight)
+        if (dweight && !a.dw)  // without rows: zeros
             k_norm_params<<<(uint32_t)ceil_div(2 * dim, 64), 64 * kSlices, 0, s>>>((const float*)workspace, (int32_t)blocks, (int32_t)dim, (P*)dweight, (P*)dbias);
     });
     return launched("scd_layer_norm_grad");

@@ -209,8 +209,10 @@ def layer_norm_grad(grad, x, mean, rstd, weight=None, params=True, out=None, str
     if params:
         need = _scratch("scd_layer_norm_grad_workspace", n, dim)
         dw, db = torch.empty((2, dim), dtype=param, device=device).unbind()
-        scratch = torch.empty(need, dtype=torch.uint8, device=device)
-        pw, pb, work = dw.data_ptr(), db.data_ptr(), scratch.data_ptr()
+        pw, pb = dw.data_ptr(), db.data_ptr()
+        if need:
+            scratch = torch.empty(need, dtype=torch.uint8, device=device)
+            work = scratch.data_ptr()
     _check(lib.scd_layer_norm_grad(grad.data_ptr(), gstride, x.data_ptr(), xstride, kind, m, r, n, dim, w, _TYPES.get(param, -1),
                                    out.data_ptr(), ostride, pw, pb, work, need, _current_stream(device.index)))
     return out, dw, db

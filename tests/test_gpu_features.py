@@ -508,3 +508,20 @@ def test_embed_grad_few_tokens_long_runs(kind, n, rows, dim):
     d = _normal(g, n, dim)
     got = features.embed_grad(t.to(DEV), d.to(DEV), rows)
     fo.close(got, fo.embed_grad(t, d, rows, 1.0, torch.float32), f"embed_grad {kind}")
+
+
+# One workgroup up to two rows for each of its groups; two rows need no workspace in any case.
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim", [(1, 5), (64, 30), (65, 30), (8, 700), (9, 700), (2, 5000), (3, 5000), (1, 33_000), (2, 33_000), (3, 33_000)])
+def test_layer_norm_gradient_of_few_rows(x, rows, dim):
+    g = _gen(rows + dim)
+    xt = TYPES[x]
+    xs, w, dy = _features_like(g, rows, dim, xt), 1 + _normal(g, dim, std=0.3), _normal(g, rows, dim, dtype=xt)
+    _, mean, rstd = features.layer_norm(xs.to(DEV), w.to(DEV))
+    want = fo.layer_norm_grad(dy, xs, mean.cpu(), rstd.cpu(), w, xt, torch.float32)
+    got = features.layer_norm_grad(dy.to(DEV), xs.to(DEV), mean, rstd, w.to(DEV))
+    for a, v, what in zip(got, want, ("x", "weight", "bias")):
+        fo.close(a, v, f"layer_norm_grad {what}")
+    xd = xs.to(DEV)
+    over = features.layer_norm_grad(dy.to(DEV), xd, mean, rstd, w.to(DEV), out=xd)
+    assert over[0] is xd and all(torch.equal(a, b) for a, b in zip(over, got))
