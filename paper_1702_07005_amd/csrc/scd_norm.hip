@@ -216,8 +216,9 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
     constexpr int kElems = LPR * NV * VEC;
     __shared__ float lds[lds_words<LPR, THREADS>(2)];
     __shared__ float part[kGroups > 1 ? kGroups * kElems : 1];
-    // The next row is loaded ahead, but not where a thread's share of the row leaves no registers for it.
-    constexpr bool kAhead = THREADS < 1024;
+    // The weights stay in registers, but not where a thread's share of the row leaves none for them: then each row reads
+    // them from the caches.
+    constexpr bool kWeights = NV * VEC <= 16;
     const int32_t lane = threadIdx.x % LPR;
     const int64_t step = (int64_t)gridDim.x * kGroups;
     const Columns<VEC, NV, LPR> col(lane, a.dim);
@@ -234,19 +235,20 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
         nmean = a.mean[row];
         nrstd = a.rstd[row];
     };
-    if (kAhead) fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
-    if (a.weight)
-#pragma unroll
-        for (int j = 0; j < NV; ++j) w[j] = load_raw<VEC>(a.weight + col.at[j]);
-    else
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
+    fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
+    const auto weights = [&](int j) {
+        if (a.weight)
+            w[j] = load_raw<VEC>(a.weight + col.at[j]);
+        else
 #pragma unroll
             for (int i = 0; i < VEC; ++i) w[j].t[i] = (P)1.0f;
+    };
+    if (kWeights)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) weights(j);
     int turn = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
         const int64_t r = r0 + threadIdx.x / LPR;
-        if (!kAhead) fetch(r);
         float dy[NV][VEC], h[NV][VEC], s[2] = {0.0f, 0.0f};
         const float mean = nmean, rstd = nrstd, here = r < a.rows ? 1.0f : 0.0f;
 #pragma unroll
@@ -254,10 +256,11 @@ __global__ void __launch_bounds__(THREADS) k_norm_grad(NormGradArgs<T, P> a) {
             widen(ndy[j], dy[j]);
             widen(nx[j], h[j]);
         }
-        if (kAhead && r0 + step < a.rows) fetch(r + step);
+        if (r0 + step < a.rows) fetch(r + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float wj[VEC];
+            if (!kWeights) weights(j);
             widen(w[j], wj);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
@@ -390,7 +393,8 @@ __global__ void __launch_bounds__(64 * kSlices) k_norm_params(const float* __res
 
 // Calls f(Int<VEC>, Int<NV>, Int<LPR>) with the smallest group that holds a row of `dim` elements of T, or returns
 // false where none does.  A wave holds four vectors a lane, but in the backward pass, which keeps six values per element,
-// of 16-bit elements three.
+// of 16-bit elements three; and the widest rows take 512 threads there, which may have 256 registers each, and 1,024 in
+// the forward pass.
 template <typename T, bool GRAD, typename F>
 bool with_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
@@ -418,15 +422,22 @@ bool with_group(int64_t dim, F&& f) {
     else if (vecs <= 1024)
         f(Int<V>{}, Int<2>{}, Int<512>{});
     else if (vecs <= 2048)
-        f(Int<V>{}, Int<2>{}, Int<1024>{});
-    else
+        f(Int<V>{}, Int<GRAD ? 4 : 2>{}, Int<GRAD ? 512 : 1024>{});
+    else if constexpr (V == 4) {
+        if (vecs > 4096) return false;
+        f(Int<V>{}, Int<GRAD ? 8 : 4>{}, Int<GRAD ? 512 : 1024>{});
+    } else {
         return false;
+    }
     return true;
 }
 
 constexpr int kNormThreads = 256;   // a workgroup, where a row's group is not wider
 constexpr int kBlocks = 2048;       // workgroups at most: eight to each CU
-constexpr int kGradBlocks = 512;    // the backward pass's, whose sums of dw and db go through memory
+// The backward pass's, whose sums of dw and db go through memory: two to a CU, or one where a row takes 512 threads, whose
+// registers fill the CU (8,192 x 8,192 in bf16: 89 us with two, 83 with one).
+constexpr int kGradBlocks = 512;
+constexpr int kGradBlocksWide = 256;
 
 template <typename F>
 void with_types(int32_t type, int32_t param, F&& f) {
@@ -516,9 +527,9 @@ extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const 
         using P = decltype(p);
         NormGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)x, x_stride, mean, rstd, (int32_t)rows, (int32_t)dim, (const P*)weight, (T*)dx, dx_stride, nullptr, nullptr, nullptr};
         int64_t blocks = 0;
-        const auto share = [&](int64_t groups) {  // the workgroups, and where their sums go
+        const auto share = [&](int64_t groups, int64_t most) {  // the workgroups, and where their sums go
             const bool alone = rows <= kTurnsAlone * groups;
-            blocks = alone && dweight ? 1 : std::min<int64_t>(kGradBlocks, ceil_div(rows, groups));
+            blocks = alone && dweight ? 1 : std::min<int64_t>(most, ceil_div(rows, groups));
             a.dw = alone ? (P*)dweight : nullptr;
             a.db = alone ? (P*)dbias : nullptr;
             a.sums = alone || !dweight ? nullptr : (float*)workspace;
@@ -526,14 +537,14 @@ extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const 
         const bool fits = rows > 0 && with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
-            share(THREADS / LPR);
+            share(THREADS / LPR, LPR >= 512 ? kGradBlocksWide : kGradBlocks);
             if (rows * dim * 3 * (int64_t)sizeof(T) < kOnceBytes)
                 k_norm_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
             else
                 k_norm_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
         });
         if (rows > 0 && !fits) {
-            share(1);
+            share(1, kGradBlocks);
             k_norm_grad_wide<<<(uint32_t)blocks, kWideThreads, 0, s>>>(a);
         }
         if (dweight && !a.dw)  // without rows: zeros
