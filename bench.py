@@ -50,7 +50,7 @@ def algorithmic_bytes(prob) -> int:
 
 
 def kernel_sources() -> list:
-    """Every file the library is compiled from: its sources and their headers."""
+    """Every file the solver is compiled from: its sources and their headers."""
     import glob
 
     from paper_1702_07005_amd import build

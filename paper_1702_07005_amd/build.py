@@ -1,4 +1,4 @@
-"""Build libscd.so (HIP, gfx950 only) in-tree.
+"""Build libscd.so (HIP, gfx950 only) and the compiled binding of its operators of learned features, in-tree.
 
     python -m paper_1702_07005_amd.build
 """
@@ -16,11 +16,17 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libscd.so")
 SOURCES = [os.path.join(CSRC, f)
            for f in ("scd_epoch.hip", "scd_hot.hip", "scd_team.hip", "scd_lock.hip", "scd_split.hip", "scd_setup.hip", "scd_probe.hip",
-                     "scd_static.hip", "scd_embed.hip", "scd_norm.hip", "scd_clip.hip",
+                     "scd_static.hip",
                      "scd_api.cpp")]
 # Measurement aid used by bench.py (device-wide atomic and copy rates); not linked into libscd.
 PROBE_LIB = os.path.join(HERE, "libscdprobe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "ceiling.hip")]
+
+# The operators of learned features: kernels of the same library, which no solver call runs.
+FEATURE_SOURCES = [os.path.join(CSRC, "features", f) for f in ("scd_embed.hip", "scd_norm.hip", "scd_clip.hip")]
+# Their binding: host code against torch's C++ headers and libscd.
+BINDING = os.path.join(HERE, "_features.so")
+BINDING_SOURCE = os.path.join(CSRC, "features", "binding.cpp")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -78,9 +84,27 @@ def _compile(sources, out, verbose):
     return out
 
 
+def _compile_binding(verbose):
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    tmp = BINDING + ".tmp"
+    includes = [sysconfig.get_paths()["include"], *cpp_extension.include_paths()]
+    _finish(_run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-Wno-unused-parameter",
+                  f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+                  *(f for p in includes for f in ("-isystem", p)), BINDING_SOURCE, "-o", tmp,
+                  *(f for p in cpp_extension.library_paths() for f in ("-L", p)), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
+                  "-L", HERE, "-l:libscd.so", "-Wl,-rpath,$ORIGIN"], verbose), verbose)
+    os.replace(tmp, BINDING)
+
+
 def build(verbose: bool = False) -> str:
     _compile(PROBE_SOURCES, PROBE_LIB, verbose)
-    return _compile(SOURCES, LIB, verbose)
+    lib = _compile([*SOURCES, *FEATURE_SOURCES], LIB, verbose)
+    _compile_binding(verbose)
+    return lib
 
 
 if __name__ == "__main__":
