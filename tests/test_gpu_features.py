@@ -525,3 +525,13 @@ def test_layer_norm_gradient_of_few_rows(x, rows, dim):
     xd = xs.to(DEV)
     over = features.layer_norm_grad(dy.to(DEV), xd, mean, rstd, w.to(DEV), out=xd)
     assert over[0] is xd and all(torch.equal(a, b) for a, b in zip(over, got))
+
+
+def test_example_trains_the_table_under_the_readout():
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import learned_features
+    objectives = learned_features.train(rounds=8, n=4096)
+    # the first read-out is fitted on random vectors; training them has to more than halve what it leaves
+    assert objectives[-1] < 0.5 * objectives[0], objectives
