@@ -188,14 +188,16 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[J], const boo
 // number of entries of its tile before it, counted: each wave compares 64 entries, one to a lane, with 64 others.
 // k_sort_merge then places every entry in the whole list: its place is the sum over the tiles of the entries before it,
 // which a binary search in each finds (those of equal key count in the tiles before its own).  A workgroup of
-// k_sort_merge holds all keys in LDS and places 64 entries, one to a lane; each of its waves searches a
+// k_sort_merge holds all keys in LDS and places kMergeEntries entries, two to a lane; each of its waves searches a
 // sixteenth of the tiles, four at a time.
 constexpr int kSmallTile = 256;
 constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
+constexpr int kMergeEntries = 128;
 
 template <typename TI>
-__global__ void __launch_bounds__(4 * kSmallTile) k_sort_tiles(Tokens<TI> src, uint32_t n, Pair* __restrict__ pairs, uint32_t tiles, Fill fill) {
+__global__ void __launch_bounds__(4 * kSmallTile) k_sort_tiles(Tokens<TI> src, uint32_t n, Pair* __restrict__ pairs,
+                                                               uint32_t* __restrict__ sorted_keys, uint32_t tiles, Fill fill) {
     if (blockIdx.x >= tiles) {
         fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
         return;
@@ -224,51 +226,65 @@ __global__ void __launch_bounds__(4 * kSmallTile) k_sort_tiles(Tokens<TI> src, u
     }
     counts[part][at] = before;
     __syncthreads();
-    if (part == 0 && i < n) pairs[blockIdx.x * kSmallTile + counts[0][at] + counts[1][at] + counts[2][at] + counts[3][at]] = p;
+    if (part == 0) {
+        const uint32_t to = blockIdx.x * kSmallTile + counts[0][at] + counts[1][at] + counts[2][at] + counts[3][at];
+        if (i < n) pairs[to] = p;
+        sorted_keys[i < n ? to : i] = keys[at];  // whole tiles
+    }
 }
 
-__global__ void __launch_bounds__(kMergeThreads) k_sort_merge(const Pair* __restrict__ in, uint32_t n, Pair* __restrict__ out,
-                                                              uint32_t own_blocks, Fill fill) {
+__global__ void __launch_bounds__(kMergeThreads) k_sort_merge(const Pair* __restrict__ in, const uint32_t* __restrict__ sorted_keys,
+                                                              uint32_t n, Pair* __restrict__ out, uint32_t own_blocks, Fill fill) {
     if (blockIdx.x >= own_blocks) {
         fill_zero(fill, blockIdx.x - own_blocks, gridDim.x - own_blocks);
         return;
     }
-    constexpr int U = 4;
+    constexpr int U = 4, E = kMergeEntries / 64;
     extern __shared__ __align__(16) uint32_t keys[];  // whole tiles, then a count per wave and entry
     const uint32_t tiles = (n + kSmallTile - 1) / kSmallTile, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     uint32_t* const counts = keys + tiles * kSmallTile;
-    const uint32_t i = blockIdx.x * 64 + lane, own = i / kSmallTile;
-    const Pair p = in[min(i, n - 1)];
-    for (uint32_t k = threadIdx.x; k < tiles * kSmallTile; k += kMergeThreads) keys[k] = k < n ? in[k].key : 0xFFFFFFFFu;
-    __syncthreads();
-    uint32_t before = 0;
-    for (uint32_t t = wave; t < tiles; t += U * kMergeWaves) {
-        uint32_t at[U];
+    // A workgroup's entries lie in one tile.
+    const uint32_t first = blockIdx.x * kMergeEntries + lane, own = blockIdx.x * kMergeEntries / kSmallTile;
+    Pair p[E];
+    uint32_t before[E] = {};
 #pragma unroll
-        for (int u = 0; u < U; ++u) at[u] = 0;
+    for (int k = 0; k < E; ++k) p[k] = in[min(first + k * 64, n - 1)];
+    for (uint32_t k = threadIdx.x; k < tiles * kSmallTile / 4; k += kMergeThreads)
+        reinterpret_cast<uint4*>(keys)[k] = reinterpret_cast<const uint4*>(sorted_keys)[k];
+    __syncthreads();
+    for (uint32_t t = wave; t < tiles; t += U * kMergeWaves) {
+        uint32_t at[U][E];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < E; ++k) at[u][k] = 0;
 #pragma unroll
         for (uint32_t step = kSmallTile / 2; step; step /= 2)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const uint32_t q = min(t + u * kMergeWaves, tiles - 1);
-                at[u] += keys[q * kSmallTile + at[u] + step - 1] < p.key + (q < own) ? step : 0;
+#pragma unroll
+                for (int k = 0; k < E; ++k) at[u][k] += keys[q * kSmallTile + at[u][k] + step - 1] < p[k].key + (q < own) ? step : 0;
             }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t q = t + u * kMergeWaves;
             if (q >= tiles || q == own) continue;
-            before += at[u] + (keys[q * kSmallTile + at[u]] < p.key + (q < own));
+#pragma unroll
+            for (int k = 0; k < E; ++k) before[k] += at[u][k] + (keys[q * kSmallTile + at[u][k]] < p[k].key + (q < own));
         }
     }
-    counts[wave * 64 + lane] = before;
-    __syncthreads();
-    if (wave == 0 && i < n) {
-        uint32_t to = i % kSmallTile;
 #pragma unroll
-        for (int w = 0; w < kMergeWaves; ++w) to += counts[w * 64 + lane];
-        out[to] = p;
+    for (int k = 0; k < E; ++k) counts[(wave * E + k) * 64 + lane] = before[k];
+    __syncthreads();
+    if (wave < E && first + wave * 64 < n) {
+        uint32_t to = (first + wave * 64) % kSmallTile;
+#pragma unroll
+        for (int w = 0; w < kMergeWaves; ++w) to += counts[(w * E + wave) * 64 + lane];
+        out[to] = wave ? p[E - 1] : p[0];
     }
 }
+static_assert(kMergeEntries == 128 && kSmallTile % kMergeEntries == 0, "two entries a lane, of one tile");
 
 // Long lists: a radix sort from the lowest digit up, a workgroup for each tile of kTileThreads x J consecutive entries.  A pass
 // counts the tiles' digits (k_sort_count), sums the counts along the tiles (k_sort_scan), and moves the entries
@@ -427,19 +443,21 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
 }
 
 // ---------------------------------------------------------------------------------------- sums
-// Group g sums entries [g S, (g+1) S) of the sorted list, run by run.  A run that lies inside is final.  Of a cut
-// run, the group where it ends keeps its piece in head[g], the groups before theirs in tail[g]; k_sums_join adds
-// them in order.  All pieces are 32 bits and unscaled.
+// A group of lanes sums `share` consecutive entries of the sorted list, run by run; a run that lies inside is final.  The
+// pieces of a run that goes over several groups of a workgroup are added in LDS by the group where it ends.  Of a run
+// that goes over several workgroups, the one where it ends keeps its piece in head[workgroup], those before theirs in
+// tail[workgroup], and k_sums_join adds them in order.  All pieces are 32 bits and unscaled.
 
 struct SumArgs {
     const Pair* pairs;
     int64_t n;
-    uint32_t share;  // S
+    uint32_t share;  // entries of a group
+    uint32_t block;  // entries of a workgroup of k_sums
     uint32_t rows;
     int32_t dim;
     float scale;
     int64_t gstride, ostride;
-    float* head;  // [groups][dim]
+    float* head;  // [workgroups of k_sums][dim]
     float* tail;
 };
 
@@ -466,49 +484,105 @@ __device__ __forceinline__ void write_row(const SumArgs& a, TO* __restrict__ out
     store_vec(p, v);
 }
 
-template <int VEC, bool ACC, typename TG, typename TO>
-__global__ void __launch_bounds__(kThreads) k_sums(SumArgs a, const TG* __restrict__ grad, TO* __restrict__ out, uint32_t log2_lanes) {
+template <int VEC, bool ACC, int THREADS, typename TG, typename TO>
+__global__ void __launch_bounds__(THREADS) k_sums(SumArgs a, const TG* __restrict__ grad, TO* __restrict__ out, uint32_t log2_lanes) {
     constexpr int U = kBatch;  // divides the share and the list
-    const int64_t g = (int64_t)blockIdx.x * (kThreads >> log2_lanes) + (threadIdx.x >> log2_lanes);
-    const int32_t col = (int32_t)((blockIdx.y << log2_lanes) + (threadIdx.x & ((1u << log2_lanes) - 1)));
-    const int64_t e0 = g * a.share, e1 = min(a.n, e0 + a.share);
-    if (e0 >= a.n || col * VEC >= a.dim) return;
+    __shared__ float tails[THREADS * VEC];
+    __shared__ uint32_t begins[THREADS / 32];  // a bit by group: what it hands on begins there (else it is a run's middle part)
+    for (uint32_t k = threadIdx.x; k < THREADS / 32; k += THREADS) begins[k] = 0;
+    __syncthreads();
+    const uint32_t j = threadIdx.x >> log2_lanes, l = threadIdx.x & ((1u << log2_lanes) - 1);
+    const int32_t col = (int32_t)((blockIdx.y << log2_lanes) + l);
+    const bool in = col * VEC < a.dim;
     int32_t again;
-    const int32_t c = vec_column<VEC>(col, a.dim, again);
-    uint32_t cur = a.pairs[e0].key;
-    bool cut = e0 > 0 && a.pairs[e0 - 1].key == cur;
-    float acc[VEC] = {};
-    for (int64_t e = e0; e < e1; e += U) {
-        const Raw<U, Pair> p = load_raw<U>(a.pairs + e);
-        Raw<VEC, TG> v[U];
+    const int32_t c = vec_column<VEC>(in ? col : 0, a.dim, again);
+    const int64_t e0 = (int64_t)blockIdx.x * a.block + j * a.share, e1 = min(a.n, e0 + a.share);
+    uint32_t cur = 0, opening = 0;
+    bool cut = false, has_head = false, more = false;
+    float acc[VEC] = {}, head[VEC] = {};
+    if (e0 < a.n) {
+        cur = opening = a.pairs[e0].key;
+        cut = e0 > 0 && a.pairs[e0 - 1].key == cur;
+        const uint32_t after = a.pairs[min(e1, a.n - 1)].key;
+        for (int64_t e = e0; e < e1; e += U) {
+            const Raw<U, Pair> p = load_raw<U>(a.pairs + e);
+            Raw<VEC, TG> v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            v[u] = load_raw_once<VEC>(grad + (int64_t)p.t[u].pos * a.gstride + c);
+            for (int u = 0; u < U; ++u) v[u] = load_raw_once<VEC>(grad + (int64_t)p.t[u].pos * a.gstride + c);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p.t[u].key != cur) {
-                if (cut)
-                    store_vec(a.head + g * a.dim + c, acc);
-                else
-                    write_row<VEC, ACC>(a, out, cur, c, again, acc);
-                cut = false;
-                cur = p.t[u].key;
+            for (int u = 0; u < U; ++u) {
+                if (p.t[u].key != cur) {
+                    if (cut) {
+                        has_head = true;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+                        for (int i = 0; i < VEC; ++i) head[i] = acc[i];
+                    } else if (in) {
+                        write_row<VEC, ACC>(a, out, cur, c, again, acc);
+                    }
+                    cut = false;
+                    cur = p.t[u].key;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+                }
+                float x[VEC];
+                widen(v[u], x);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[i] += x[i];
             }
-            float x[VEC];
-            widen(v[u], x);
+        }
+        if (cur < a.rows) {
+            more = e1 < a.n && after == cur;
+            if (!more && cut) {
+                has_head = true;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] += x[i];
+                for (int i = 0; i < VEC; ++i) head[i] = acc[i];
+            } else if (!more && in) {
+                write_row<VEC, ACC>(a, out, cur, c, again, acc);
+            }
         }
     }
-    if (cur >= a.rows) return;
-    if (e1 < a.n && a.pairs[e1].key == cur)
-        store_vec(a.tail + g * a.dim + c, acc);
-    else if (cut)
-        store_vec(a.head + g * a.dim + c, acc);
-    else
-        write_row<VEC, ACC>(a, out, cur, c, again, acc);
+    if (l == 0 && !(more && cut)) atomicOr(&begins[j / 32], 1u << j % 32);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) tails[threadIdx.x * VEC + i] = acc[i];
+    __syncthreads();
+    // Adds the pieces of the run that group j - 1 hands on, from the group where it begins; true where that lies before the
+    // workgroup.
+    const auto add_before = [&](float (&s)[VEC]) {
+        int32_t word = (int32_t)j / 32;
+        uint32_t bits = begins[word] & ((1u << j % 32) - 1);
+        while (!bits && word > 0) bits = begins[--word];
+        const bool open = !bits;
+        for (uint32_t k = open ? 0 : word * 32 + 31 - __builtin_clz(bits); k < j; k += U) {
+            float x[U][VEC];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) x[u][i] = tails[((min(k + u, j - 1) << log2_lanes) + l) * VEC + i];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[i] += k + u < j ? x[u][i] : 0.0f;
+        }
+        return open;
+    };
+    if (!in) return;
+    if (has_head) {
+        float s[VEC] = {};
+        const bool open = add_before(s);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[i] += head[i];
+        if (open)
+            store_vec(a.head + (int64_t)blockIdx.x * a.dim + c, s);
+        else
+            write_row<VEC, ACC>(a, out, opening, c, again, s);
+    }
+    if (more && j == (THREADS >> log2_lanes) - 1) {  // the run goes on in the next workgroup
+        float s[VEC] = {};
+        if (cut) add_before(s);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[i] += acc[i];
+        store_vec(a.tail + (int64_t)blockIdx.x * a.dim + c, s);
+    }
 }
 
 // The sum of tail[first], tail[first + step], ... below `end`, for the vector at column c.
@@ -527,12 +601,12 @@ __device__ __forceinline__ void add_tails(const SumArgs& a, int64_t first, int64
     }
 }
 
-// The group in which the run that covers the start of group g (and the entry before it) begins.  The starts of the
-// groups 1, 2, 4, ... before are looked at, several together, then the range between two of them in eighths.
+// The workgroup of k_sums in which the run that covers the start of its workgroup g (and the entry before it) begins.  The
+// starts of the workgroups 1, 2, 4, ... before are looked at, several together, then the range between two of them in eighths.
 __device__ __forceinline__ int64_t run_begins(const SumArgs& a, int64_t g, uint32_t row) {
     constexpr int P = 8;
     const auto covers = [&](int64_t k, uint32_t key) { return k > 0 && key == row; };
-    const auto before = [&](int64_t k) { return a.pairs[max(k, (int64_t)1) * a.share - 1].key; };
+    const auto before = [&](int64_t k) { return a.pairs[max(k, (int64_t)1) * a.block - 1].key; };
     int64_t in = g, out = 0;  // the run covers the start of `in`; once out < in, not that of `out`
     bool more = true;
     const auto probe = [&](auto probes, int64_t step) {  // looks at g - step, g - 2 step, g - 4 step, ... together
@@ -557,7 +631,7 @@ __device__ __forceinline__ int64_t run_begins(const SumArgs& a, int64_t g, uint3
         probe(Int<P>{}, step);
         step <<= P;
     }
-    while (in - out > 1) {  // the run's first entry lies in a group from `out` to in - 1
+    while (in - out > 1) {  // the run's first entry lies in a workgroup from `out` to in - 1
         const int64_t lo = out, size = in - out;
         uint32_t key[P - 1];
 #pragma unroll
@@ -576,9 +650,9 @@ __device__ __forceinline__ int64_t run_begins(const SumArgs& a, int64_t g, uint3
     return out;
 }
 
-// A row's pieces are joined by their last group where they are few.  Of more pieces, each of the m groups of a wave (or,
-// where a wave has one group or the run is very long, of the workgroup) adds every m-th, and the m sums are added in
-// a fixed order.
+// A group of lanes for each workgroup of k_sums: where a run ends there that began before, it joins the run's pieces.  Of
+// many pieces, each of the m groups of its wave (or, where a wave has one group or the run is very long, of its workgroup)
+// adds every m-th, and the m sums are added in a fixed order.
 template <int VEC, bool ACC, int THREADS, typename TO>
 __global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict__ out, uint32_t log2_lanes) {
     __shared__ float part[THREADS * VEC];
@@ -589,7 +663,7 @@ __global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict
     const bool in = col * VEC < a.dim;
     int32_t again;
     const int32_t c = vec_column<VEC>(in ? col : 0, a.dim, again);
-    const int64_t e0 = g * a.share, e1 = min(a.n, e0 + a.share);
+    const int64_t e0 = g * a.block, e1 = min(a.n, e0 + a.block);
     int64_t begin = -1;
     uint32_t row = 0;
     if (e0 > 0 && e0 < a.n) {
@@ -644,7 +718,7 @@ __global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict
             load_vec(a.head + end * a.dim + c, h);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s[i] += h[i];
-            write_row<VEC, ACC>(a, out, a.pairs[end * a.share].key, c, again, s);
+            write_row<VEC, ACC>(a, out, a.pairs[end * a.block].key, c, again, s);
         }
         __syncthreads();
     }
@@ -801,7 +875,6 @@ struct Plan {
     int per_thread;
     int64_t tiles;
     uint32_t share;
-    int64_t groups;
     int64_t pairs;    // bytes of one list
     int64_t hist, pieces, bytes;
 };
@@ -831,10 +904,11 @@ Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     // Entries per group: as many as keep about 4,096 waves in work, 8 at least, 64 at most.
     const int64_t work = p.n * ceil_div(dim, 4) / 64;
     p.share = (uint32_t)std::min<int64_t>(64, std::max<int64_t>(8, work / 4096 / 8 * 8));
-    p.groups = ceil_div(p.n, p.share);
     p.pairs = align16(p.n * sizeof(Pair));
-    p.hist = p.tiled ? 0 : align16(((p.tiles + 1) << p.bits) * 4);
-    p.pieces = align16(p.groups * dim * 4);
+    // The tiles' keys, or the counts of digits and their totals.
+    p.hist = p.tiled ? ceil_div(p.n, kSmallTile) * kSmallTile * 4 : align16(((p.tiles + 1) << p.bits) * 4);
+    // The pieces of runs: a row for each workgroup of k_sums, which has one group at least.
+    p.pieces = align16(ceil_div(p.n, p.share) * dim * 4);
     p.bytes = 2 * p.pairs + p.hist + 2 * p.pieces;
     return p;
 }
@@ -854,17 +928,17 @@ Fill fill_part(const Fill& f, int64_t part, int64_t parts) {
 
 // Leaves the sorted list in `pairs`; `other` is scratch.
 template <typename TI>
-int sort_short(Tokens<TI> src, const Plan& p, Pair* pairs, Pair* other, const Fill& fill, hipStream_t s) {
-    const uint32_t tiles = (uint32_t)ceil_div(p.n, kSmallTile), blocks = (uint32_t)ceil_div(p.n, 64);
+int sort_short(Tokens<TI> src, const Plan& p, Pair* pairs, Pair* other, uint32_t* keys, const Fill& fill, hipStream_t s) {
+    const uint32_t tiles = (uint32_t)ceil_div(p.n, kSmallTile), blocks = (uint32_t)ceil_div(p.n, kMergeEntries);
     Fill part = fill_part(fill, 0, 2);
-    k_sort_tiles<<<tiles + fill_blocks(part, 4 * kSmallTile), 4 * kSmallTile, 0, s>>>(src, (uint32_t)p.n, other, tiles, part);
-    const size_t lds = (size_t)(tiles * kSmallTile + kMergeThreads) * 4;
+    k_sort_tiles<<<tiles + fill_blocks(part, 4 * kSmallTile), 4 * kSmallTile, 0, s>>>(src, (uint32_t)p.n, other, keys, tiles, part);
+    const size_t lds = (size_t)(tiles * kSmallTile + kMergeWaves * kMergeEntries) * 4;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_merge), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return fail(SCD_ERR_HIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
     }
     part = fill_part(fill, 1, 2);
-    k_sort_merge<<<blocks + fill_blocks(part, kMergeThreads), kMergeThreads, lds, s>>>(other, (uint32_t)p.n, pairs, blocks, part);
+    k_sort_merge<<<blocks + fill_blocks(part, kMergeThreads), kMergeThreads, lds, s>>>(other, keys, (uint32_t)p.n, pairs, blocks, part);
     return launched("sort of tokens");
 }
 
@@ -983,7 +1057,7 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         const Tokens<TI> src{(const TI*)tokens, n, (uint32_t)rows};
         Pair* const other = (Pair*)(w + p.pairs);
         if (p.tiled) {
-            rc = sort_short(src, p, pairs, other, fill, s);
+            rc = sort_short(src, p, pairs, other, (uint32_t*)(w + 2 * p.pairs), fill, s);
             return;
         }
         // The passes' launches share the zeros evenly.
@@ -1020,19 +1094,21 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         using TO = decltype(to);
         constexpr int VEC = decltype(vc)::value;
         const RowMap m = row_map(dim, VEC);
-        const dim3 grid((uint32_t)ceil_div(p.groups, kThreads >> m.log2_lanes), m.ranges);
-        const auto go = [&](auto acc) {
+        const auto go = [&](auto acc, auto threads) {
             constexpr bool ACC = decltype(acc)::value;
-            k_sums<VEC, ACC><<<grid, kThreads, 0, s>>>(a, (const TG*)grad, (TO*)out, m.log2_lanes);
-            const auto join = [&](auto threads) {
-                constexpr int THREADS = decltype(threads)::value;
-                const dim3 blocks((uint32_t)ceil_div(p.groups, THREADS >> m.log2_lanes), m.ranges);
-                k_sums_join<VEC, ACC, THREADS><<<blocks, THREADS, 0, s>>>(a, (TO*)out, m.log2_lanes);
-            };
-            // Wide rows get workgroups of several groups all the same.
-            m.log2_lanes >= 6 ? join(Int<1024>{}) : join(Int<kThreads>{});
+            constexpr int THREADS = decltype(threads)::value;
+            const int64_t groups = THREADS >> m.log2_lanes;
+            a.block = (uint32_t)(p.share * groups);
+            const int64_t blocks = ceil_div(p.n, a.block);
+            const dim3 grid((uint32_t)blocks, m.ranges), join((uint32_t)ceil_div(blocks, groups), m.ranges);
+            k_sums<VEC, ACC, THREADS><<<grid, THREADS, 0, s>>>(a, (const TG*)grad, (TO*)out, m.log2_lanes);
+            if (blocks > 1) k_sums_join<VEC, ACC, THREADS><<<join, THREADS, 0, s>>>(a, (TO*)out, m.log2_lanes);
         };
-        accumulate ? go(std::true_type{}) : go(std::false_type{});
+        // Wide rows get workgroups of several groups all the same.
+        if (m.log2_lanes >= 6)
+            accumulate ? go(std::true_type{}, Int<1024>{}) : go(std::false_type{}, Int<1024>{});
+        else
+            accumulate ? go(std::true_type{}, Int<kThreads>{}) : go(std::false_type{}, Int<kThreads>{});
     });
     return launched("scd_embed_grad");
 }
