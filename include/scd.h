@@ -386,12 +386,12 @@ int scd_embed(const void *tokens_dev, int32_t token_type, int64_t n, const void 
               int64_t out_stride, void *stream);
 
 /* The gradient of scd_embed with respect to its table: out[v, :] = scale * sum of grad[t, :] over the t with
- * tokens[t] = v, in ascending order of t up to the split of long runs; rows without a token get zeros, tokens
- * outside [0, rows) add to nothing (their gradients are not read).  accumulate = 1 adds this to what out
+ * tokens[t] = v, in an order that the sizes alone fix (long runs are split); rows without a token get zeros, tokens
+ * outside [0, rows) add to nothing, whatever their gradients hold.  accumulate = 1 adds this to what out
  * holds, and leaves rows without a token as they are.
  *   grad_dev: [n, dim];  out_dev: [rows, dim], of any element type.
- * The tokens are sorted first (a stable radix sort), so that each row is summed by its owner and written
- * once, without atomics.  scd_embed_grad_workspace gives the bytes of scratch that a call needs (16-byte
+ * The tokens are sorted first, stably, so that each row is summed by its owner and written once, without
+ * floating-point atomics.  scd_embed_grad_workspace gives the bytes of scratch that a call needs (16-byte
  * aligned, device; 0 for short lists). */
 int scd_embed_grad_workspace(int64_t n, int64_t rows, int64_t dim, int64_t *bytes);
 int scd_embed_grad(const void *tokens_dev, int32_t token_type, int64_t n, const void *grad_dev, int32_t grad_type,

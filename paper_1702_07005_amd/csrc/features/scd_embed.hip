@@ -3,12 +3,13 @@
 // Lookup: out[t] = s E[tok[t]].  Gradient: dE[v] = s sum_{t: tok[t]=v} g[t].  Both only move data: the
 // lookup reads the rows in use once and writes n rows; the gradient reads n rows and writes the whole table.
 //
-// The gradient sorts (token, position) pairs by token with a stable radix sort, so that the rows of one token
-// are consecutive and in ascending position; every run of equal tokens is then summed in registers and its
-// row written once.  Runs are cut where a group's share of the sorted list ends; the pieces of a cut run
-// go through the workspace in 32 bits and are added in order.  No atomics: results are bit-identical from
-// call to call.  The zeros of the rows without a token are written while the sort, which moves
-// little data, runs.
+// The gradient sorts (token, position) pairs by token, stably, so that the rows of one token are consecutive and in
+// ascending position; every run of equal tokens is then summed in registers and its row written once.  Runs are cut
+// where a group of lanes or a workgroup has its share of the list; the pieces are added in 32 bits in an order that the
+// sizes alone fix.  No floating-point atomics: results are bit-identical from call to call.  The zeros of the rows
+// without a token are written by further workgroups of the sort's launches, which move little data themselves.
+// Three ways to the sorted list, by its length: none at all (k_grad_few), tiles ordered by counting and merged
+// (k_sort_tiles, k_sort_merge), a radix sort (k_sort_count, k_sort_scan, k_sort_move).
 #include <algorithm>
 #include <type_traits>
 

@@ -16,6 +16,12 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 PAIRS = [(a, b) for a in TYPES for b in TYPES]
 
 
+@pytest.fixture(scope="module", autouse=True)
+def _give_back_memory():
+    yield
+    torch.cuda.empty_cache()
+
+
 def _gen(seed):
     return torch.Generator().manual_seed(seed)
 
