@@ -771,6 +771,16 @@ __global__ void __launch_bounds__(kFewThreads) k_grad_few(Tokens<TI> src, SumArg
         atomicOr(&given[key / 32], 1u << key % 32);
     }
     __syncthreads();
+    const auto fill_others = [&] {
+        if (ACC || !in) return;
+        const float zero[VEC] = {};
+        for (uint32_t r = j; r < here; r += m)
+            if (!(given[r / 32] >> r % 32 & 1)) store_vec(out + (int64_t)(r0 + r) * a.ostride + c, zero);
+    };
+    if (count == 0) {
+        fill_others();
+        return;
+    }
     if (i < count) {  // its place: how many of the keys before it in the list are at most its key, and of those after it less
         const uint32_t own = keys[i], wave = i / 64;
         uint32_t to = 0;
@@ -793,11 +803,7 @@ __global__ void __launch_bounds__(kFewThreads) k_grad_few(Tokens<TI> src, SumArg
     if (start) starts[at] = i;
     if (i == 0) starts[runs] = count;
     __syncthreads();
-    if (!ACC && in) {
-        const float zero[VEC] = {};
-        for (uint32_t r = j; r < here; r += m)
-            if (!(given[r / 32] >> r % 32 & 1)) store_vec(out + (int64_t)(r0 + r) * a.ostride + c, zero);
-    }
+    fill_others();  // after the last barrier of the ordering, which would wait for the stores
     const auto add = [&](uint32_t from, uint32_t end, uint32_t step, float (&s)[VEC]) {
         for (uint32_t e = from; e < end; e += U * step) {
             Raw<VEC, TG> v[U];

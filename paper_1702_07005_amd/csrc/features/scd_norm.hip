@@ -460,11 +460,12 @@ int check_norm(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {
 
 int64_t grad_blocks(int64_t rows) { return std::min<int64_t>(rows, kGradBlocks); }
 
-// Up to this many rows for each group of a workgroup, one workgroup does it all, which saves the second launch; a call of
-// so few rows needs no workspace, whatever its groups.
-constexpr int64_t kTurnsAlone = 2;
+// Up to this many rows for each group of a workgroup, one workgroup does it all, which saves the second launch: 9 rows of 851
+// (bf16) 10.4 us with two launches, 7.0 with one.  A row of 512 threads takes longer than the launch (4 rows of 8,505 in
+// fp32 27 us alone): there one row.  A call of one row needs no workspace, whatever its groups.
+constexpr int64_t kTurnsAlone = 4;
 
-int64_t grad_workspace(int64_t rows, int64_t dim) { return rows <= kTurnsAlone ? 0 : grad_blocks(rows) * 2 * dim * 4; }
+int64_t grad_workspace(int64_t rows, int64_t dim) { return rows <= 1 ? 0 : grad_blocks(rows) * 2 * dim * 4; }
 
 }  // namespace
 }  // namespace feat
@@ -527,8 +528,8 @@ extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const 
         using P = decltype(p);
         NormGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)x, x_stride, mean, rstd, (int32_t)rows, (int32_t)dim, (const P*)weight, (T*)dx, dx_stride, nullptr, nullptr, nullptr};
         int64_t blocks = 0;
-        const auto share = [&](int64_t groups, int64_t most) {  // the workgroups, and where their sums go
-            const bool alone = rows <= kTurnsAlone * groups;
+        const auto share = [&](int64_t groups, int64_t most, int64_t turns) {  // the workgroups, and where their sums go
+            const bool alone = rows <= turns * groups;
             blocks = alone && dweight ? 1 : std::min<int64_t>(most, ceil_div(rows, groups));
             a.dw = alone ? (P*)dweight : nullptr;
             a.db = alone ? (P*)dbias : nullptr;
@@ -537,14 +538,14 @@ extern "C" int scd_layer_norm_grad(const void* grad, int64_t grad_stride, const 
         const bool fits = rows > 0 && with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kNormThreads ? LPR : kNormThreads;
-            share(THREADS / LPR, LPR >= 512 ? kGradBlocksWide : kGradBlocks);
+            share(THREADS / LPR, LPR >= 512 ? kGradBlocksWide : kGradBlocks, LPR >= 512 ? 1 : kTurnsAlone);
             if (rows * dim * 3 * (int64_t)sizeof(T) < kOnceBytes)
                 k_norm_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
             else
                 k_norm_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
         });
         if (rows > 0 && !fits) {
-            share(1, kGradBlocks);
+            share(1, kGradBlocks, 1);
             k_norm_grad_wide<<<(uint32_t)blocks, kWideThreads, 0, s>>>(a);
         }
         if (dweight && !a.dw)  // without rows: zeros

@@ -516,7 +516,7 @@ def test_embed_grad_few_tokens_long_runs(kind, n, rows, dim):
     fo.close(got, fo.embed_grad(t, d, rows, 1.0, torch.float32), f"embed_grad {kind}")
 
 
-# One workgroup up to two rows for each of its groups; two rows need no workspace in any case.
+# One workgroup does few rows for each of its groups alone; one row needs no workspace in any case.
 @pytest.mark.parametrize("x", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,dim", [(1, 5), (64, 30), (65, 30), (8, 700), (9, 700), (2, 5000), (3, 5000), (1, 33_000), (2, 33_000), (3, 33_000)])
 def test_layer_norm_gradient_of_few_rows(x, rows, dim):
