@@ -541,3 +541,18 @@ def test_example_trains_the_table_under_the_readout():
     objectives = learned_features.train(rounds=8, n=4096)
     # the first read-out is fitted on random vectors; training them has to more than halve what it leaves
     assert objectives[-1] < 0.5 * objectives[0], objectives
+
+
+@pytest.mark.parametrize("n", [1, 40, 1000])
+def test_embed_grad_few_tokens_into_a_large_table(n):
+    # zeros by pieces of memory: rows of an odd width, in two column ranges, before, between and after the tokens' rows
+    g = _gen(n)
+    rows, dim = 16_001, 1051
+    t = torch.randint(0, rows, (n,), generator=g)
+    t[0] = rows - 1
+    if n > 2:
+        t[1:3] = torch.tensor([0, 1])
+    d = _normal(g, n, dim)
+    out = torch.full((rows, dim), float("nan"), device=DEV)
+    features.embed_grad(t.to(DEV), d.to(DEV), rows, out=out)
+    fo.close(out, fo.embed_grad(t, d, rows, 1.0, torch.float32), "embed_grad")
