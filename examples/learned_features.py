@@ -2,11 +2,11 @@
 
 Documents are lists of term ids (Zipf's law, of unequal lengths, the rest of a row padded with -1), each with a
 label that its terms' hidden weights give.  A document's features are the mean of its terms' normalised
-vectors.  A round looks the terms up, normalises their vectors, fits the read-out by coordinate descent from
+vectors.  An iteration looks the terms up, normalises their vectors, fits the read-out by coordinate descent from
 where it stood, and takes one step of gradient descent on the table and the norm's parameters, clipped by the
 norm of all three gradients together:
 
-    python examples/learned_features.py [--rounds 12] [--documents 8192]
+    python examples/learned_features.py [--iterations 12] [--documents 8192]
 """
 from __future__ import annotations
 
@@ -33,8 +33,8 @@ def documents(n, length, terms, seed):
     return ids.masked_fill_(~there, -1), (label - label.mean()) / label.std()
 
 
-def train(rounds=12, n=8192, length=48, terms=3000, dim=64, lam=1e-3, rate=20.0, max_norm=0.2, seed=0, report=None):
-    """The primal objective of the fitted read-out in each round."""
+def train(iterations=12, n=8192, length=48, terms=3000, dim=64, lam=1e-3, rate=20.0, max_norm=0.2, seed=0, report=None):
+    """The primal objective of the fitted read-out in each iteration."""
     ids, label = documents(n, length, terms, seed)
     there = (ids >= 0).unsqueeze(2)
     share = there / there.sum(1, keepdim=True)  # of each place in its document's features
@@ -47,7 +47,7 @@ def train(rounds=12, n=8192, length=48, terms=3000, dim=64, lam=1e-3, rate=20.0,
     idx = torch.arange(n, dtype=torch.int32, device="cuda").repeat(dim)
     readout = torch.zeros(dim, device="cuda")
     objectives = []
-    for k in range(rounds):
+    for k in range(iterations):
         x = features.embed(ids, table, scale=scale)
         y, mean, rstd = features.layer_norm(x, weight, bias)
         docs = (y * share).sum(1)
@@ -67,13 +67,13 @@ def train(rounds=12, n=8192, length=48, terms=3000, dim=64, lam=1e-3, rate=20.0,
         for p, d in zip((table, weight, bias), grads):
             p.sub_(d, alpha=rate if p is table else 1.0)
         if report:
-            report(f"round {k}: primal objective {primal:.6f}, gap {primal - dual:.1e}, gradient norm {float(norm):.4f}")
+            report(f"iteration {k}: primal objective {primal:.6f}, gap {primal - dual:.1e}, gradient norm {float(norm):.4f}")
     return objectives
 
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    ap.add_argument("--rounds", type=int, default=12)
+    ap.add_argument("--iterations", type=int, default=12)
     ap.add_argument("--documents", type=int, default=8192)
     a = ap.parse_args()
-    train(rounds=a.rounds, n=a.documents, report=lambda line: print(line, flush=True))
+    train(iterations=a.iterations, n=a.documents, report=lambda line: print(line, flush=True))

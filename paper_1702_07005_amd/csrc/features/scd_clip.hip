@@ -6,6 +6,9 @@
 // workgroup takes a run of consecutive chunks.  Squares are summed in 64 bits: the square of a 32-bit value
 // overflows 32 bits, and the 64-bit units are idle otherwise.  Each workgroup of the first kernel writes its sum; every
 // workgroup of the second adds them all in the same order (a few KB from the cache) and scales its share.
+//
+// Measured: 354 M weights from bf16 to fp32 490 us (2.1 GB that it cannot do without: 4.3 TB/s; with what is read twice
+// and not from the cache, 5.4); 11 tensors of 160,000 weights in all 9.9 us, two launches.
 #include <algorithm>
 #include <cmath>
 

