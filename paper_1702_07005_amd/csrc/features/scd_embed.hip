@@ -122,9 +122,9 @@ __device__ __forceinline__ void fill_bytes(char* p, int64_t bytes, int64_t worke
 }
 
 __device__ __forceinline__ void fill_zero(const Fill& f, uint32_t block, uint32_t blocks) {
-    if (f.stride == f.row_bytes) {  // a run of whole 64-byte lines for each workgroup
-        const int64_t total = f.rows * f.row_bytes, share = (total / blocks + 63) / 64 * 64, from = min(total, block * share);
-        fill_bytes(f.p + from, min(share, total - from), threadIdx.x, blockDim.x);
+    if (f.stride == f.row_bytes) {
+        const Piece piece = fill_piece(f.rows * f.row_bytes, block, blocks);
+        fill_bytes(f.p + piece.from, piece.bytes, threadIdx.x, blockDim.x);
         return;
     }
     const int64_t waves = (int64_t)blocks * (blockDim.x / 64);

@@ -11,6 +11,7 @@
 
 #include "scd.h"
 #include "scd_kernels.h"
+#include "scd_plan.h"
 
 namespace scd {
 namespace feat {
@@ -146,15 +147,6 @@ inline void with_type(int32_t t, F&& f) {
 
 constexpr int64_t kMaxDim = int64_t(1) << 20;
 constexpr int64_t kMaxRows = 2147483647LL;
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// log2 of the smallest power of two that is at least n.
-inline uint32_t log2_up(uint64_t n) {
-    uint32_t l = 0;
-    while ((uint64_t(1) << l) < n) ++l;
-    return l;
-}
 
 }  // namespace feat
 }  // namespace scd

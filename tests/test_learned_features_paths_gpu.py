@@ -1,0 +1,47 @@
+"""The operators of learned features on the GPU, at sizes chosen by the code that they reach: every sort of the
+lookup gradient, every join of its sums, loads and stores past the caches, second turns of the row loops, whole chunks
+of the clipping.  Outputs hold NaN before the call, so that an element that is not written shows."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import _features_oracle as fo  # noqa: E402
+from paper_1702_07005_amd import features  # noqa: E402
+
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _give_back_memory():
+    yield
+    torch.cuda.empty_cache()
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _nan(*shape, dtype=torch.float32):
+    return torch.full(shape, float("nan"), dtype=dtype, device=DEV)
+
+
+# ---------------------------------------------------------------- zeros of the lookup gradient
+
+
+# Tables whose zeros, shared out among workgroups in whole 64-byte lines, leave a remainder: the last bytes of each
+# launch's part lie in rows without tokens.
+@pytest.mark.parametrize("n,rows,dim,dtype,spare", [
+    (2_000, 52_000, 300, torch.float32, (25_999, 51_999)), (20_000, 52_000, 300, torch.float32, (25_999, 51_999)),
+    (2_000, 57_000, 255, torch.float32, (28_499, 56_999)), (100_000, 3_000, 333, torch.bfloat16, (499, 1_499, 1_999, 2_999))])
+def test_embed_grad_zeros_reach_the_end_of_every_part(n, rows, dim, dtype, spare):
+    g = _gen(n + rows)
+    t = torch.randint(0, rows, (n,), generator=g)
+    for r in spare:
+        t[t == r] = 0
+    d = torch.randn(n, dim, generator=g).to(dtype)
+    out = features.embed_grad(t.to(DEV), d.to(DEV), rows, out=_nan(rows, dim, dtype=dtype))
+    fo.close(out, fo.embed_grad(t, d, rows, 1.0, dtype), "embed_grad")
