@@ -23,22 +23,6 @@ namespace scd {
 namespace feat {
 namespace {
 
-constexpr int kThreads = 256;
-
-// A row is `lanes` consecutive threads (a power of two, at most 256) with VEC elements each, and as many
-// such column ranges (blockIdx.y) as it needs.  Rows narrower than 16 bytes go element by element (VEC = 1).
-struct RowMap {
-    uint32_t log2_lanes;
-    uint32_t ranges;
-};
-
-RowMap row_map(int64_t dim, int vec) {
-    RowMap m;
-    m.log2_lanes = std::min<uint32_t>(8, log2_up((uint64_t)ceil_div(dim, vec)));
-    m.ranges = (uint32_t)ceil_div(dim, (int64_t)vec << m.log2_lanes);
-    return m;
-}
-
 // ---------------------------------------------------------------------------------------- lookup
 
 // A large output goes past the caches (ONCE), so that the table's rows stay there.  2.6 M ids into 1.5 M x 16 (fp32, 164 MB
@@ -80,11 +64,10 @@ __global__ void __launch_bounds__(kThreads) k_embed(const TI* __restrict__ tok, 
 // Keys are the tokens; one outside [0, rows) gets the key `rows` and so comes last.  The list is padded to a whole
 // number of batches of k_sums with such keys, at position 0.
 
-constexpr int kBatch = 8;
-
 struct __align__(8) Pair {
     uint32_t key, pos;
 };
+static_assert(sizeof(Pair) == kPairBytes);
 
 template <typename TI>
 struct Tokens {
@@ -195,7 +178,6 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[J], const boo
 // which a binary search in each finds (those of equal key count in the tiles before its own).  A workgroup of
 // k_sort_merge holds all keys in LDS and places kMergeEntries entries, two to a lane; each of its waves searches a
 // sixteenth of the tiles, four at a time.
-constexpr int kSmallTile = 256;
 constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
 constexpr int kMergeEntries = 128;
@@ -296,9 +278,7 @@ static_assert(kMergeEntries == 128 && kSmallTile % kMergeEntries == 0, "two entr
 // (k_sort_move), which orders its tile in LDS first, so that it writes runs of consecutive entries.  Every launch
 // fills a part of the zeros with further workgroups.  The move is bound by its tiles' counters (one for each wave and
 // digit): 1.28 M entries in digits of 11 bits take 17 to 20 us, in which their stores take 3.
-constexpr int kTileThreads = 512;
 constexpr int kTileWaves = kTileThreads / 64;
-constexpr int kMaxBits = 11;
 constexpr int kPer = (1 << kMaxBits) / kTileThreads;  // digits a thread at most: k_sort_move gives it consecutive ones
 
 template <int J, typename SRC>
@@ -747,7 +727,6 @@ __global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict
 // range), picks the tokens that lie in them, orders them by counting, fills the other rows with zeros and sums the runs,
 // long ones with several groups.  Every workgroup reads all tokens, so this is for lists that cost less than
 // the launches of a sort.
-constexpr int kFewMax = 1024;
 constexpr int kFewThreads = 1024;
 constexpr int kFewRows = 16384;  // of a workgroup at most: a bit each in LDS
 constexpr int64_t kFlatBytes = int64_t(64) << 20;
@@ -906,53 +885,6 @@ void with_vec(int32_t a, int32_t b, int64_t dim, F&& f) {
 bool is_element(int32_t t) { return type_bytes(t) != 0; }
 bool is_token(int32_t t) { return t == SCD_I32 || t == SCD_I64; }
 
-// How a gradient call sorts and splits: a function of the sizes alone.
-struct Plan {
-    bool few;         // no sorted list: nothing below is used
-    int64_t n;        // padded to whole batches
-    bool tiled;       // a short list
-    int passes, bits;
-    int per_thread;
-    int64_t tiles;
-    uint32_t share;
-    int64_t pairs;    // bytes of one list
-    int64_t hist, pieces, bytes;
-};
-
-// Lists of up to this many entries are sorted by tiles, or up to twice as many where the radix sort takes several passes.
-// Whole calls: 16,384 tokens into 1,000 x 256 (one pass) 28 us by tiles and 35 by radix, 30,000 46 and 38;
-// 30,000 into 300,000 x 64 (two passes) 47 and 58, 16,384 into 75,000 x 1,024 46 and 71.
-constexpr int64_t kTiledMax = 16384;
-
-int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
-
-Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
-    Plan p{};
-    p.few = n <= kFewMax;
-    if (p.few) return p;
-    p.n = ceil_div(n, kBatch) * kBatch;
-    const int key_bits = std::max(1, (int)log2_up((uint64_t)rows + 1));
-    // Digits of 9 bits, or of up to 11 where that saves a pass: the more digits, the shorter the runs that a tile writes.
-    p.passes = std::min((key_bits + 8) / 9, (key_bits + kMaxBits - 1) / kMaxBits);
-    p.tiled = p.n <= kTiledMax * (p.passes > 1 ? 2 : 1);
-    p.bits = (key_bits + p.passes - 1) / p.passes;
-    // Entries of a tile's thread: enough tiles for the CUs while the list is short, few counts of digits where it is long.
-    // Whole calls with 2, 4 and 8: 131,072 into 50,000 x 512 74, 77 and 84 us; 300,000 into 1.5 M x 32 78, 76 and 84;
-    // 600,000 into 1.5 M x 16 96, 89 and 90; 1.28 M into 1.5 M x 16 (4 and 8) 135 and 120.
-    p.per_thread = p.n <= 200'000 ? 2 : p.n <= 800'000 ? 4 : 8;
-    p.tiles = ceil_div(p.n, kTileThreads * p.per_thread);
-    // Entries per group: as many as keep about 4,096 waves in work, 8 at least, 64 at most.
-    const int64_t work = p.n * ceil_div(dim, 4) / 64;
-    p.share = (uint32_t)std::min<int64_t>(64, std::max<int64_t>(8, work / 4096 / 8 * 8));
-    p.pairs = align16(p.n * sizeof(Pair));
-    // The tiles' keys, or the counts of digits and their totals.
-    p.hist = p.tiled ? ceil_div(p.n, kSmallTile) * kSmallTile * 4 : align16(((p.tiles + 1) << p.bits) * 4);
-    // The pieces of runs: a row for each workgroup of k_sums, which has one group at least.
-    p.pieces = align16(ceil_div(p.n, p.share) * dim * 4);
-    p.bytes = 2 * p.pairs + p.hist + 2 * p.pieces;
-    return p;
-}
-
 // Workgroups of `threads` threads that fill a part of the zeros beside other work: 64 bytes a thread, but at most 2 M
 // threads in all.
 uint32_t fill_blocks(const Fill& f, int threads) {
@@ -1009,10 +941,8 @@ extern "C" int scd_embed(const void* tokens, int32_t token_type, int64_t n, cons
     if (!tokens || (!table && rows > 0) || !out) return fail(SCD_ERR_INVALID, "null device pointer");
     const int vec = vec_for(table_type, out_type, dim);
     const RowMap m = row_map(dim, vec);
-    const int64_t per = kThreads >> m.log2_lanes;
-    // Four rows per thread in flight once that still leaves eight workgroups to each CU.
-    const int U = ceil_div(n, per * 4) * m.ranges >= 2048 ? 4 : 1;
-    const dim3 grid((uint32_t)ceil_div(n, per * U), m.ranges);
+    const int U = embed_unroll(n, m);
+    const int64_t most = embed_tokens(m, U);
     with_vec(table_type, out_type, dim, [&](auto tt, auto to, auto vc) {
         using TT = decltype(tt);
         using TO = decltype(to);
@@ -1020,8 +950,13 @@ extern "C" int scd_embed(const void* tokens, int32_t token_type, int64_t n, cons
         const auto go = [&](auto ti, auto uc, auto once) {
             using TI = decltype(ti);
             constexpr int U = decltype(uc)::value;
-            k_embed<VEC, U, decltype(once)::value><<<grid, kThreads, 0, (hipStream_t)stream>>>((const TI*)tokens, n, (const TT*)table, table_stride, rows,
-                                                                                             (int32_t)dim, scale, (TO*)out, out_stride, m.log2_lanes);
+            for (int64_t from = 0; from < n; from += most) {
+                const int64_t here = std::min(most, n - from);
+                const dim3 grid((uint32_t)ceil_div(here, (kThreads >> m.log2_lanes) * U), m.ranges);
+                k_embed<VEC, U, decltype(once)::value><<<grid, kThreads, 0, (hipStream_t)stream>>>(
+                    (const TI*)tokens + from, here, (const TT*)table, table_stride, rows, (int32_t)dim, scale, (TO*)out + from * out_stride, out_stride,
+                    m.log2_lanes);
+            }
         };
         const auto with_ids = [&](auto ti) {
             if (U == 1)

@@ -44,3 +44,43 @@ def test_pieces_of_zeros_cover_every_byte_once(tmp_path):
                 }
             }
     return 0;""")
+
+
+def test_no_launch_exceeds_what_the_gpu_takes(tmp_path):
+    # Every launch whose size grows with the call's: fewer than 2^32 threads along an axis, up to 2^31 - 1 tokens and rows.
+    out = _run(tmp_path, r"""
+    const int64_t limit = int64_t(1) << 32, sizes[] = {1, 1025, 200'000, 67'108'860, 67'108'861, 70'000'000, 134'217'729, 1'073'741'695, 1'073'741'697, 1'073'741'825, 2'147'483'647};
+    int64_t most = 0, slices = 0, shares = 0;
+    for (int64_t n : sizes)
+        for (int64_t dim : {1, 3, 7, 8, 9, 65, 130, 257, 513, 516, 1025, 4100, 1 << 20})
+            for (int vec : {1, 4, 8}) {
+                if (vec == 1 ? dim >= 8 : dim < vec) continue;
+                const RowMap m = row_map(dim, vec);
+                const int unroll = embed_unroll(n, m);
+                const int64_t tokens = embed_tokens(m, unroll);
+                const int64_t blocks = ceil_div(std::min(n, tokens), (kThreads >> m.log2_lanes) * unroll);
+                if (tokens < 1 || blocks * kThreads >= limit || m.ranges > 65535) {
+                    printf("BAD lookup n=%lld dim=%lld vec=%d\n", (long long)n, (long long)dim, vec);
+                    return 1;
+                }
+                most = std::max(most, blocks * kThreads);
+                slices = std::max(slices, ceil_div(n, tokens));
+                const Plan p = plan_for(n, 1000, dim);
+                if (p.few) continue;
+                for (int64_t threads : {256, 512}) {
+                    const int64_t groups = threads >> m.log2_lanes, sums = ceil_div(p.n, p.share * groups);
+                    if (p.share % kBatch || sums * threads >= limit || ceil_div(sums, groups) * threads >= limit) {
+                        printf("BAD sums n=%lld dim=%lld vec=%d\n", (long long)n, (long long)dim, vec);
+                        return 1;
+                    }
+                }
+                shares = std::max<int64_t>(shares, p.share);
+                if (p.tiles * kTileThreads + (1 << 21) >= limit) {
+                    printf("BAD sort n=%lld\n", (long long)n);
+                    return 1;
+                }
+            }
+    printf("%lld %lld %lld\n", (long long)(most >> 20), (long long)slices, (long long)shares);
+    return 0;""")
+    most, slices, shares = map(int, out.split())
+    assert most >= 4000 and slices > 1 and shares > 64, out  # the limits were reached

@@ -29,6 +29,23 @@ def _nan(*shape, dtype=torch.float32):
     return torch.full(shape, float("nan"), dtype=dtype, device=DEV)
 
 
+# ---------------------------------------------------------------- lookup
+
+
+def test_embed_more_tokens_than_one_launch_takes():
+    # Rows of 256 lanes: a launch takes 67,108,860 tokens at four for each workgroup.
+    n, rows, dim = 67_108_860 + 1_001, 2_000, 1025
+    if torch.cuda.mem_get_info()[0] < 2 * n * dim + (8 << 30):
+        pytest.skip("needs 146 GB of GPU memory")
+    g = torch.Generator(device=DEV).manual_seed(1)
+    table = torch.randn(rows, dim, generator=g, device=DEV).bfloat16()
+    t = torch.randint(-1, rows, (n,), generator=g, device=DEV, dtype=torch.int32)
+    out = features.embed(t, table)
+    full = torch.cat([table, torch.zeros(1, dim, dtype=table.dtype, device=DEV)])  # -1 is its last row
+    for at in range(0, n, 1 << 20):
+        assert torch.equal(out[at:at + (1 << 20)], full[t[at:at + (1 << 20)].long()]), at
+
+
 # ---------------------------------------------------------------- zeros of the lookup gradient
 
 
