@@ -91,10 +91,11 @@ inline Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     if (p.few) return p;
     p.n = ceil_div(n, kBatch) * kBatch;
     const int key_bits = std::max(1, (int)log2_up((uint64_t)rows + 1));
-    // Digits of 9 bits, or of up to 11 where that saves a pass: the more digits, the shorter the runs that a tile writes.
-    p.passes = std::min((key_bits + 8) / 9, (key_bits + kMaxBits - 1) / kMaxBits);
+    // As few passes as digits of at most 11 bits take, which share the key's bits evenly: the more digits, the shorter the
+    // runs that a tile writes.
+    p.passes = (int)ceil_div(key_bits, kMaxBits);
     p.tiled = p.n <= kTiledMax * (p.passes > 1 ? 2 : 1);
-    p.bits = (key_bits + p.passes - 1) / p.passes;
+    p.bits = (int)ceil_div(key_bits, p.passes);
     // Entries of a tile's thread: enough tiles for the CUs while the list is short, few counts of digits where it is long.
     // Whole calls with 2, 4 and 8: 131,072 into 50,000 x 512 74, 77 and 84 us; 300,000 into 1.5 M x 32 78, 76 and 84;
     // 600,000 into 1.5 M x 16 96, 89 and 90; 1.28 M into 1.5 M x 16 (4 and 8) 135 and 120.

@@ -84,3 +84,17 @@ def test_no_launch_exceeds_what_the_gpu_takes(tmp_path):
     return 0;""")
     most, slices, shares = map(int, out.split())
     assert most >= 4000 and slices > 1 and shares > 64, out  # the limits were reached
+
+
+def test_radix_digits_take_the_whole_key_in_the_fewest_passes(tmp_path):
+    out = _run(tmp_path, r"""
+    for (int key = 1; key <= 31; ++key) {
+        const Plan p = plan_for(1'000'000, (int64_t(1) << key) - 1, 16);  // keys are rows and the number of rows
+        if (p.tiled || p.bits > kMaxBits || p.bits * p.passes < key || (p.passes - 1) * kMaxBits >= key) {
+            printf("BAD key=%d passes=%d bits=%d\n", key, p.passes, p.bits);
+            return 1;
+        }
+        printf("%d,%d ", p.passes, p.bits);
+    }
+    return 0;""").split()
+    assert [out[k - 1] for k in (1, 11, 12, 21, 22, 23, 27, 31)] == ["1,1", "1,11", "2,6", "2,11", "2,11", "3,8", "3,9", "3,11"]
