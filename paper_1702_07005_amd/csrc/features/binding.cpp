@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/Allocator.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -127,16 +128,34 @@ at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Device& d
     return at::empty(sizes, at::TensorOptions().dtype(type).device(device));
 }
 
+// The calls are outside autograd: they record nothing.  A caller's tensor that they write to counts the write, as
+// after an in-place operation of torch, so that autograd notices where it had saved the former values; and one whose own
+// history would no longer hold is refused.
+void check_writable(const at::Tensor& t, const std::string& what) {
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        refuse(what + " requires gradients, which writing to it would make wrong: call under torch.no_grad(), or detach it");
+}
+
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The output of a call: `out` if given, else a new tensor of `type`.
 struct Output {
     at::Tensor t;
     Rows rows;
+    bool given;
+    void done() const {
+        if (given) written(t);
+    }
 };
 
 Output output(const Call& c, int out, at::IntArrayRef sizes, at::ScalarType type, const at::Device& device) {
     Output o;
-    if (c.given(out)) {
+    o.given = c.given(out);
+    if (o.given) {
         o.t = c.tensor(out, "out");
+        check_writable(o.t, "out");
         if (o.t.sizes() != sizes || o.t.scalar_type() != type || o.t.device() != device)
             refuse(std::string("out must have the result's shape and device and the type ") + c10::toString(type));
     } else {
@@ -188,6 +207,7 @@ PyObject* embed(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Output o = output(c, 3, shape_of(tokens.sizes(), t.dim), result_type(c, 4, 3, table.scalar_type()), table.device());
     check(scd_embed(tokens.data_ptr(), ids, tokens.numel(), t.data, t.type, t.stride, table.size(0), t.dim, Call::real(c.args[2]),
                     o.rows.data, o.rows.type, o.rows.stride, c.stream));
+    o.done();
     return THPVariable_Wrap(o.t);
     END_HANDLE_TH_ERRORS
 }
@@ -211,6 +231,7 @@ PyObject* embed_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Scratch work(need);
     check(scd_embed_grad(tokens.data_ptr(), ids, g.n, g.data, g.type, g.stride, rows, g.dim, Call::real(c.args[3]), accumulate,
                          o.rows.data, o.rows.type, o.rows.stride, work.data.get(), need, c.stream));
+    o.done();
     return THPVariable_Wrap(o.t);
     END_HANDLE_TH_ERRORS
 }
@@ -231,6 +252,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor mean = fresh(lead, at::kFloat, device), rstd = fresh(lead, at::kFloat, device);
     check(scd_layer_norm(r.data, r.type, r.stride, r.n, r.dim, w, b, element(param), Call::real(c.args[3]), o.rows.data, o.rows.stride,
                          static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), c.stream));
+    o.done();
     return Py_BuildValue("(NNN)", THPVariable_Wrap(o.t), THPVariable_Wrap(mean), THPVariable_Wrap(rstd));
     END_HANDLE_TH_ERRORS
 }
@@ -262,6 +284,7 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check(scd_layer_norm_grad(g.data, g.stride, r.data, r.stride, r.type, static_cast<const float*>(m), static_cast<const float*>(s), r.n, r.dim, w,
                               element(param), o.rows.data, o.rows.stride, params ? dw.data_ptr() : nullptr, params ? db.data_ptr() : nullptr,
                               work.data.get(), need, c.stream));
+    o.done();
     if (!params) return Py_BuildValue("(NOO)", THPVariable_Wrap(o.t), Py_None, Py_None);
     return Py_BuildValue("(NNN)", THPVariable_Wrap(o.t), THPVariable_Wrap(dw), THPVariable_Wrap(db));
     END_HANDLE_TH_ERRORS
@@ -291,6 +314,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
             refuse("gradient " + std::to_string(i) + " must be a contiguous float32, bfloat16 or float16 tensor on the first one's GPU");
         scd_span_t& s = spans[(size_t)i];
         s = scd_span_t{g.data_ptr(), in_place ? g.data_ptr() : nullptr, g.numel(), type, type};
+        if (in_place) check_writable(g, "gradient " + std::to_string(i));
         if (!outs) continue;
         PyObject* const q = PySequence_Fast_GET_ITEM(outs.get(), i);
         if (!THPVariable_Check(q)) refuse("out must be tensors");
@@ -298,6 +322,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
         s.dst_type = element(o.scalar_type());
         if ((s.dst_type != type && s.dst_type != SCD_F32) || o.device() != device || o.sizes() != g.sizes() || !o.is_contiguous())
             refuse("output " + std::to_string(i) + " must be contiguous, with its gradient's shape and device, and its type or float32");
+        check_writable(o, "output " + std::to_string(i));
         s.dst = o.data_ptr();
     }
     if (device.index() != c.device) return none();
@@ -306,6 +331,8 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor norm = fresh({}, at::kFloat, device);
     const Scratch work(need);
     check(scd_clip_grads(spans.data(), count, Call::real(c.args[2]), static_cast<float*>(norm.data_ptr()), work.data.get(), need, c.stream));
+    if (in_place || outs)
+        for (Py_ssize_t i = 0; i < count; ++i) written(THPVariable_Unpack(PySequence_Fast_GET_ITEM((in_place ? grads : outs).get(), i)));
     return THPVariable_Wrap(norm);
     END_HANDLE_TH_ERRORS
 }

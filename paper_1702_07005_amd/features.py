@@ -11,6 +11,11 @@ Matrices may be views with any row stride, but their last dimension has unit str
 the current stream, or on ``stream`` (a torch stream or a raw handle), with which the caller orders the
 inputs; outputs that the call allocates then belong to that stream.
 
+The operators are outside autograd: they record nothing, results never require gradients, and backward passes are
+calls of their own.  Tensors that a call writes to (``out``, gradients clipped in place) count it as an in-place
+operation, so that autograd refuses a backward pass that needs their former values; one that itself requires gradients is
+refused unless gradients are off (``torch.no_grad()``).
+
     x = features.embed(ids, table, scale=table.shape[1] ** 0.5)
     y, mean, rstd = features.layer_norm(x, weight, bias)
     dx, dw, db = features.layer_norm_grad(dy, x, mean, rstd, weight)

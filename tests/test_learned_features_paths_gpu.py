@@ -62,3 +62,71 @@ def test_embed_grad_zeros_reach_the_end_of_every_part(n, rows, dim, dtype, spare
     d = torch.randn(n, dim, generator=g).to(dtype)
     out = features.embed_grad(t.to(DEV), d.to(DEV), rows, out=_nan(rows, dim, dtype=dtype))
     fo.close(out, fo.embed_grad(t, d, rows, 1.0, dtype), "embed_grad")
+
+
+# ---------------------------------------------------------------- beside autograd
+
+
+def _writes(x, y, grads):
+    """Calls that write to x (out, accumulation, in place) or to the gradients."""
+    ids = torch.arange(6, device=DEV)
+    n = x.shape[1]
+    _, mean, rstd = features.layer_norm(y)
+    yield x, lambda: features.embed(ids, y, out=x)
+    yield x, lambda: features.embed_grad(ids, y, 6, out=x)
+    yield x, lambda: features.embed_grad(ids, y, 6, out=x, accumulate=True)
+    yield x, lambda: features.layer_norm(y, torch.ones(n, device=DEV), out=x)
+    yield x, lambda: features.layer_norm(x, out=x)
+    yield x, lambda: features.layer_norm_grad(y, y, mean, rstd, out=x)
+    yield grads[1], lambda: features.clip_grads(grads, 1e-3)
+    yield x, lambda: features.clip_grads(grads[:1], 1e-3, out=[x])
+
+
+def _six():
+    return torch.randn(6, 8, device=DEV)
+
+
+def test_writes_count_as_in_place_operations():
+    x, y, grads = _six(), _six(), [_six(), _six()]
+    for k, (to, call) in enumerate(_writes(x, y, grads)):
+        before, others, view = to._version, (y._version, grads[0]._version), to[1:3]
+        call()
+        assert to._version > before and view._version == to._version, k
+        if k != 6:
+            assert (y._version, grads[0]._version) == others, k
+    before = [g._version for g in grads]
+    features.grad_norm(grads)
+    assert [g._version for g in grads] == before
+    with torch.inference_mode():
+        z = _six()
+    for to, call in _writes(z, y, [z, z.clone()]):
+        call()
+
+
+def test_autograd_notices_overwritten_values():
+    for k in range(8):
+        x, grads = _six(), [_six(), _six()]
+        to, call = list(_writes(x, _six(), grads))[k]
+        p = _six().requires_grad_()
+        loss = (p * to).sum()
+        call()
+        with pytest.raises(RuntimeError, match="in-?place"):
+            loss.backward()
+
+
+def test_tensors_that_require_gradients():
+    table = _six().requires_grad_()
+    got = features.embed(torch.arange(6, device=DEV), table)
+    assert not got.requires_grad and torch.equal(got, table)
+    for k in range(8):
+        for leaf in (True, False):
+            x = _six().requires_grad_() if leaf else _six().requires_grad_() * 2
+            grads = [_six(), _six().requires_grad_() if leaf else _six().requires_grad_() * 2]
+            to, call = list(_writes(x, _six(), grads))[k]
+            before = to.detach().clone()
+            with pytest.raises(ValueError, match="requires gradients"):
+                call()
+            assert torch.equal(to, before)
+            with torch.no_grad():
+                call()
+            assert not torch.equal(to, before), k
