@@ -8,6 +8,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -60,7 +61,7 @@ def _finish(proc, verbose):
     noise = "is not a recognized feature for this target"
     err = "\n".join(line for line in stderr.splitlines() if noise not in line)
     if proc.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({proc.returncode}):\n{err}")
+        raise RuntimeError(f"{proc.args[0]} failed ({proc.returncode}):\n{err}")
     if verbose and err.strip():
         print(err, file=sys.stderr)
 
@@ -84,9 +85,19 @@ def _compile(sources, out, verbose):
     return out
 
 
-def _compile_binding(verbose):
-    import sysconfig
+def _binding_lacks() -> list:
+    """What the binding is compiled with and is not installed; the library and its C interface need none of it."""
+    import importlib.util
 
+    spec = importlib.util.find_spec("torch")
+    headers = {"Python.h": sysconfig.get_paths()["include"]}
+    if spec and spec.origin:
+        headers["torch/csrc/autograd/python_variable.h"] = os.path.join(os.path.dirname(spec.origin), "include")
+    lacks = [h for h, where in headers.items() if not os.path.exists(os.path.join(where, h))]
+    return lacks + [what for what, there in (("torch", spec), ("g++", shutil.which("g++"))) if not there]
+
+
+def _compile_binding(verbose):
     import torch
     from torch.utils import cpp_extension
 
@@ -103,7 +114,13 @@ def _compile_binding(verbose):
 def build(verbose: bool = False) -> str:
     _compile(PROBE_SOURCES, PROBE_LIB, verbose)
     lib = _compile([*SOURCES, *FEATURE_SOURCES], LIB, verbose)
-    _compile_binding(verbose)
+    lacks = _binding_lacks()
+    if lacks:
+        print(f"the binding of features.py is not built: no {', '.join(lacks)}", file=sys.stderr)
+        if os.path.exists(BINDING):
+            os.remove(BINDING)  # it may not fit the library
+    else:
+        _compile_binding(verbose)
     return lib
 
 
