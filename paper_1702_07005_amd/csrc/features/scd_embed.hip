@@ -824,7 +824,7 @@ __global__ void __launch_bounds__(kFewThreads) k_grad_few(Tokens<TI> src, SumArg
     constexpr uint32_t kLong = 2 * U;  // entries that a group sums alone
     for (uint32_t q = j; q < runs && in; q += m) {
         const uint32_t from = starts[q], end = starts[q + 1];
-        if (end - from > kLong && m > 1) continue;
+        if (end - from > kLong) continue;
         float s[VEC] = {};
         add(from, end, 1, s);
         write_row<VEC, ACC>(a, out, r0 + sorted[from].key, c, again, s);
@@ -843,7 +843,7 @@ __global__ void __launch_bounds__(kFewThreads) k_grad_few(Tokens<TI> src, SumArg
         }
         return;
     }
-    if (m == 1) return;
+    // m is from 4 to 16 here, less than such a run has entries.
     for (uint32_t q = 0; q < runs; ++q) {
         const uint32_t from = starts[q], end = starts[q + 1];
         if (end - from <= kLong) continue;
@@ -853,8 +853,7 @@ __global__ void __launch_bounds__(kFewThreads) k_grad_few(Tokens<TI> src, SumArg
         for (int k = 0; k < VEC; ++k) part[i * VEC + k] = s[k];
         __syncthreads();
         if (j == 0 && in) {
-            const uint32_t parts = min(m, end - from);
-            for (uint32_t k = 1; k < parts; ++k)
+            for (uint32_t k = 1; k < m; ++k)
 #pragma unroll
                 for (int v = 0; v < VEC; ++v) s[v] += part[((k << log2_lanes) + l) * VEC + v];
             write_row<VEC, ACC>(a, out, r0 + sorted[from].key, c, again, s);
