@@ -1075,16 +1075,14 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
         const auto go = [&](auto acc, auto threads) {
             constexpr bool ACC = decltype(acc)::value;
             constexpr int THREADS = decltype(threads)::value;
-            const int64_t groups = THREADS >> m.log2_lanes;
+            const int64_t groups = THREADS >> m.log2_lanes, blocks = sums_blocks(p.n, p.share, m);
             a.block = (uint32_t)(p.share * groups);
-            const int64_t blocks = ceil_div(p.n, a.block);
             const dim3 grid((uint32_t)blocks, m.ranges), join((uint32_t)ceil_div(blocks, groups), m.ranges);
             k_sums<VEC, ACC, THREADS><<<grid, THREADS, 0, s>>>(a, (const TG*)grad, (TO*)out, m.log2_lanes);
             if (blocks > 1) k_sums_join<VEC, ACC, THREADS><<<join, THREADS, 0, s>>>(a, (TO*)out, m.log2_lanes);
         };
-        // Wide rows get workgroups of several groups all the same.
-        if (m.log2_lanes >= 6)
-            accumulate ? go(std::true_type{}, Int<512>{}) : go(std::false_type{}, Int<512>{});
+        if (sums_threads(m) == kWideSums)
+            accumulate ? go(std::true_type{}, Int<kWideSums>{}) : go(std::false_type{}, Int<kWideSums>{});
         else
             accumulate ? go(std::true_type{}, Int<kThreads>{}) : go(std::false_type{}, Int<kThreads>{});
     });

@@ -65,6 +65,13 @@ constexpr Piece fill_piece(int64_t total, int64_t block, int64_t blocks) {
     return Piece{from, share < total - from ? share : total - from};
 }
 
+// Threads of a workgroup of the sums (k_sums): wide rows get workgroups of several groups of lanes all the same.
+constexpr int kWideSums = 512;
+inline int sums_threads(const RowMap& m) { return m.log2_lanes >= 6 ? kWideSums : kThreads; }
+
+// Workgroups of the sums of n entries, of which each group of lanes takes `share`.
+inline int64_t sums_blocks(int64_t n, uint32_t share, const RowMap& m) { return ceil_div(n, (int64_t)share * (sums_threads(m) >> m.log2_lanes)); }
+
 // How a gradient call sorts and splits: a function of the sizes alone.
 struct Plan {
     bool few;         // no sorted list: nothing below is used
@@ -110,8 +117,11 @@ inline Plan plan_for(int64_t n, int64_t rows, int64_t dim) {
     p.pairs = align16(p.n * kPairBytes);
     // The tiles' keys, or the counts of digits and their totals.
     p.hist = p.tiled ? ceil_div(p.n, kSmallTile) * kSmallTile * 4 : align16(((p.tiles + 1) << p.bits) * 4);
-    // The pieces of runs: a row for each workgroup of k_sums, which has one group at least.
-    p.pieces = align16(ceil_div(p.n, p.share) * dim * 4);
+    // The pieces of runs: a row for each workgroup of the sums, as many as there are with vectors of 1, 4 or 8 elements.
+    int64_t blocks = dim < 8 ? sums_blocks(p.n, p.share, row_map(dim, 1)) : 0;
+    for (int vec = 4; vec <= 8; vec += 4)
+        if (dim >= vec) blocks = std::max(blocks, sums_blocks(p.n, p.share, row_map(dim, vec)));
+    p.pieces = align16(blocks * dim * 4);
     p.bytes = 2 * p.pairs + p.hist + 2 * p.pieces;
     return p;
 }

@@ -98,3 +98,28 @@ def test_radix_digits_take_the_whole_key_in_the_fewest_passes(tmp_path):
     }
     return 0;""").split()
     assert [out[k - 1] for k in (1, 11, 12, 21, 22, 23, 27, 31)] == ["1,1", "1,11", "2,6", "2,11", "2,11", "3,8", "3,9", "3,11"]
+
+
+def test_workspace_of_the_sums_holds_their_pieces_and_little_more(tmp_path):
+    # A row of 32 bits for each workgroup, whichever the element types (16 bytes of the wider one are a vector).
+    _run(tmp_path, r"""
+    for (int64_t n : {1025, 1100, 16'384, 32'769, 300'000, 1'277'952, 50'000'001})
+        for (int64_t dim : {1, 2, 3, 4, 5, 7, 8, 9, 12, 16, 17, 31, 33, 64, 65, 127, 128, 255, 256, 257, 300, 511, 513, 1000, 1024, 1025, 1055, 2047, 2049, 4096, 8193, 1 << 20}) {
+            const Plan p = plan_for(n, 1'000'000, dim);
+            int64_t most = 0;
+            for (int bytes : {2, 4}) {
+                const int vec = 16 / bytes;
+                const RowMap m = row_map(dim, dim < vec ? 1 : vec);
+                const int64_t blocks = sums_blocks(p.n, p.share, m), groups = sums_threads(m) >> m.log2_lanes;
+                if (groups < 1 || blocks * p.share * groups < p.n || (blocks - 1) * p.share * groups >= p.n) {
+                    printf("BAD blocks n=%lld dim=%lld bytes=%d\n", (long long)n, (long long)dim, bytes);
+                    return 1;
+                }
+                most = std::max(most, blocks * dim * 4);
+            }
+            if (p.pieces < most || p.pieces > most + 15 || p.bytes != 2 * p.pairs + p.hist + 2 * p.pieces) {
+                printf("BAD pieces n=%lld dim=%lld: %lld of %lld\n", (long long)n, (long long)dim, (long long)p.pieces, (long long)most);
+                return 1;
+            }
+        }
+    return 0;""")
