@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+import _features_sizes as sizes
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PLANS = os.path.join(ROOT, "paper_1702_07005_amd", "csrc", "features")
 
@@ -123,3 +125,39 @@ def test_workspace_of_the_sums_holds_their_pieces_and_little_more(tmp_path):
             }
         }
     return 0;""")
+
+
+def _braces(rows):
+    return "{" + ", ".join("{" + ", ".join(map(str, r)) + "}" for r in rows) + "}"
+
+
+def test_listed_sizes_take_the_routes_they_are_listed_for(tmp_path):
+    sorts = [(n, rows, dim) for _, n, rows, dim in sizes.SORTS]
+    sums = [r[1:] for r in sizes.SUMS]
+    out = _run(tmp_path, f"""
+    const int64_t sorts[][3] = {_braces(sorts)}, sums[][4] = {_braces(sums)}, runs[][4] = {_braces(sizes.LONG_RUNS)},
+                  lookups[][4] = {_braces([r[1:] for r in sizes.LOOKUPS])};""" + r"""
+    const auto map = [](int64_t dim, int64_t bytes) { return row_map(dim, dim < 16 / bytes ? 1 : int(16 / bytes)); };
+    for (const auto& t : sorts) {
+        const Plan p = plan_for(t[0], t[1], t[2]);
+        if (p.few) return 1;
+        if (p.tiled)
+            printf("tiles %d\n", p.passes);
+        else
+            printf("radix%d %d\n", p.per_thread, p.passes);
+    }
+    for (const auto& t : sums) {
+        const RowMap m = map(t[2], t[3]);
+        if (plan_for(t[0], t[1], t[2]).few) return 1;
+        printf("%d %d %u\n", sums_threads(m), sums_threads(m) >> m.log2_lanes, m.ranges);
+    }
+    for (const auto& t : runs) {  // a workgroup joins more than 32 pieces for each group of a wave, or 16 where it has one
+        const RowMap m = map(t[2], t[3]);
+        const Plan p = plan_for(t[0], t[1], t[2]);
+        const int64_t beside = m.log2_lanes < 6 ? 64 >> m.log2_lanes : 1;
+        printf("%d\n", !p.few && sums_blocks(p.n, p.share, m) - 1 > (beside > 1 ? 32 * beside : 16));
+    }
+    for (const auto& t : lookups) printf("%d\n", embed_unroll(t[0], map(t[2], t[3])));
+    return 0;""").splitlines()
+    want = [r[0] for r in sizes.SORTS] + ["%d %d %d" % r[0] for r in sizes.SUMS] + ["1"] * len(sizes.LONG_RUNS) + [str(r[0]) for r in sizes.LOOKUPS]
+    assert out == want, [(a, b) for a, b in zip(out, want) if a != b]

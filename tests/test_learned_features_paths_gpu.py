@@ -10,9 +10,11 @@ if not torch.cuda.is_available():
     pytest.skip("needs a GPU", allow_module_level=True)
 
 import _features_oracle as fo  # noqa: E402
+import _features_sizes as sizes  # noqa: E402
 from paper_1702_07005_amd import features  # noqa: E402
 
 DEV = "cuda"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -27,6 +29,35 @@ def _gen(seed):
 
 def _nan(*shape, dtype=torch.float32):
     return torch.full(shape, float("nan"), dtype=dtype, device=DEV)
+
+
+def _on_gpu(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _matrix(g, rows, dim, dtype, pad=0, offset=0, std=1.0):
+    """Normal values in a view whose rows lie `pad` elements further apart and begin `offset` elements into the memory."""
+    room = _nan(offset + rows * (dim + pad), dtype=dtype)
+    v = room[offset:].view(rows, dim + pad)[:, :dim]
+    v.copy_(torch.randn(rows, dim, generator=g, device=DEV) * std)
+    return v
+
+
+def _blank(rows, dim, dtype, pad, offset):
+    return _nan(offset + rows * (dim + pad), dtype=dtype)[offset:].view(rows, dim + pad)[:, :dim]
+
+
+def _gaps_untouched(v):
+    """The elements between the rows of a view made here still are NaN."""
+    return bool(torch.isnan(v.as_strided((v.shape[0], v.stride(0)), (v.stride(0), 1))[:, v.shape[1]:]).all())
+
+
+def _close(got, want, what):
+    """`fo.close` for values on the GPU."""
+    value, bound = want
+    off = (got.double().reshape(value.shape) - value).abs()  # NaN where either is
+    if not bool((off <= bound).all()):
+        fo.close(got, (value.cpu(), bound.cpu()), what)
 
 
 # ---------------------------------------------------------------- lookup
@@ -46,6 +77,36 @@ def test_embed_more_tokens_than_one_launch_takes():
         assert torch.equal(out[at:at + (1 << 20)], full[t[at:at + (1 << 20)].long()]), at
 
 
+@pytest.mark.parametrize("unroll,n,rows,dim,width", sizes.LOOKUPS)
+def test_embed_rows_in_flight(unroll, n, rows, dim, width):
+    g = _gen(n + dim)
+    table, to = (F32, BF16) if width == 4 else (F16, F16)
+    t = torch.randint(-2, rows + 2, (n,), generator=g)
+    e = torch.randn(rows, dim, generator=g).to(table)
+    for ids in (torch.int64, torch.int32):
+        got = features.embed(t.to(DEV, ids), e.to(DEV), scale=0.7, out=_nan(n, dim, dtype=to))
+        fo.close(got, fo.embed(t, e, float(torch.tensor(0.7)), to), "embed")
+
+
+# More than 96 MB of output is written past the caches: 2-byte aligned vectors and odd widths, and rows narrower than a
+# vector.  Bit for bit the same as in pieces that are not.
+@pytest.mark.parametrize("table,to,n,rows,dim", [(BF16, F32, 200_003, 5_000, 131), (F32, F32, 26_001, 900, 1_030), (BF16, BF16, 130_001, 4_000, 401),
+                                                 (F32, F16, 391_001, 3_000, 129), (F16, F16, 10_500_001, 300, 5), (F32, F32, 8_400_001, 300, 3)])
+def test_embed_past_the_caches(table, to, n, rows, dim):
+    g = _on_gpu(n + dim)
+    e = _matrix(g, rows, dim, table, pad=3, offset=1)
+    t = torch.randint(-2, rows + 2, (n,), generator=g, device=DEV)
+    out = _blank(n, dim, to, 1, 3)
+    assert n * dim * out.element_size() >= 96 << 20
+    got = features.embed(t, e, scale=1.3, out=out)
+    assert got is out and _gaps_untouched(out)
+    for at in range(0, n, n // 4):
+        part = features.embed(t[at:at + n // 4], e, scale=1.3, dtype=to)
+        assert torch.equal(torch.isnan(part), torch.isnan(out[at:at + n // 4])), at
+        assert torch.equal(part.nan_to_num(), out[at:at + n // 4].nan_to_num()), at
+    fo.close(out[:2000], fo.embed(t[:2000].cpu(), e.cpu(), float(torch.tensor(1.3)), to), "embed")
+
+
 # ---------------------------------------------------------------- zeros of the lookup gradient
 
 
@@ -62,6 +123,194 @@ def test_embed_grad_zeros_reach_the_end_of_every_part(n, rows, dim, dtype, spare
     d = torch.randn(n, dim, generator=g).to(dtype)
     out = features.embed_grad(t.to(DEV), d.to(DEV), rows, out=_nan(rows, dim, dtype=dtype))
     fo.close(out, fo.embed_grad(t, d, rows, 1.0, dtype), "embed_grad")
+
+
+# ---------------------------------------------------------------- sorts and sums of the lookup gradient
+
+
+def _tokens(g, n, rows, kind):
+    if kind == "one":
+        t = torch.full((n,), rows // 2)
+    else:
+        u = torch.rand(n, generator=g, dtype=torch.float64)
+        t = (torch.exp(u * torch.log(torch.tensor(rows + 1.0))) - 1).long().clamp(0, rows - 1)
+        t[torch.rand(n, generator=g) < 0.02] = -1
+        t[torch.rand(n, generator=g) < 0.01] = rows
+        t[:2] = torch.tensor([rows - 1, 0])
+    return t
+
+
+def _gradients(g, t, rows, dim, dtype):
+    """Gradients that hold NaN at tokens without a row."""
+    d = torch.randn(t.numel(), dim, generator=g).to(dtype)
+    d[(t < 0) | (t >= rows)] = float("nan")
+    return d
+
+
+@pytest.mark.parametrize("kind", ["zipf", "one"])
+@pytest.mark.parametrize("route,n,rows,dim", sizes.SORTS)
+def test_embed_grad_sorts(route, n, rows, dim, kind):
+    g = _gen(n + rows)
+    t = _tokens(g, n, rows, kind)
+    d = _gradients(g, t, rows, dim, F32)
+    out = features.embed_grad(t.to(DEV), d.to(DEV), rows, out=_nan(rows, dim))
+    fo.close(out, fo.embed_grad(t, d, rows, 1.0, F32), f"embed_grad {route}")
+
+
+@pytest.mark.parametrize("kind", ["zipf", "one"])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("workgroup,n,rows,dim,width", sizes.SUMS)
+def test_embed_grad_sums(workgroup, n, rows, dim, width, accumulate, kind):
+    g = _gen(n + rows + dim)
+    grad, to = (F16, F32) if width == 4 else (BF16, BF16)
+    t = _tokens(g, n, rows, kind)
+    d = _gradients(g, t, rows, dim, grad)
+    before = torch.randn(rows, dim, generator=g).to(to) if accumulate else None
+    out = _blank(rows, dim, to, 5, 1)
+    if accumulate:
+        out.copy_(before)
+    features.embed_grad(t.int().to(DEV), d.to(DEV), rows, scale=-1.5, out=out, accumulate=accumulate)
+    assert _gaps_untouched(out)
+    fo.close(out, fo.embed_grad(t, d, rows, -1.5, to, before), "embed_grad")
+
+
+@pytest.mark.parametrize("n,rows,dim,width", sizes.LONG_RUNS)
+def test_embed_grad_long_runs(n, rows, dim, width):
+    g = _gen(n + rows + dim)
+    dtype = F32 if width == 4 else BF16
+    t = _tokens(g, n, rows, "one")
+    t[: n // 50] = torch.arange(n // 50) % rows  # and some for the rows around it
+    d = _gradients(g, t, rows, dim, dtype)
+    out = features.embed_grad(t.to(DEV), d.to(DEV), rows, out=_nan(rows, dim, dtype=dtype))
+    fo.close(out, fo.embed_grad(t, d, rows, 1.0, dtype), "embed_grad")
+    again = features.embed_grad(t.to(DEV), d.to(DEV), rows)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("n", [3_000, 70_000])
+def test_embed_grad_of_one_gradient_for_all_tokens(n):
+    g = _gen(n)
+    t = _tokens(g, n, 900, "zipf")
+    t[t == 900] = -1
+    one = torch.randn(1, 24, generator=g)
+    out = features.embed_grad(t.to(DEV), one.to(DEV).expand(n, 24), 900, out=_nan(900, 24))
+    fo.close(out, fo.embed_grad(t, one.expand(n, 24), 900, 1.0, F32), "embed_grad")
+
+
+# ---------------------------------------------------------------- layer norm, turns of the row loops
+
+
+def _norm_inputs(seed, rows, dim, dtype, param, pad, offset):
+    g = _on_gpu(seed)
+    x = _matrix(g, rows, dim, dtype, pad, offset)
+    x.mul_((0.1 + 2 * torch.rand(rows, 1, generator=g, device=DEV)).to(dtype)).add_(0.4)
+    w = (1 + 0.3 * torch.randn(dim, generator=g, device=DEV)).to(param)
+    b = torch.randn(dim, generator=g, device=DEV).to(param)
+    return x, w, b, _matrix(g, rows, dim, dtype, pad + 1, offset + 2)
+
+
+def _check_norm(rows, dim, dtype, param, pad=0, offset=0):
+    x, w, b, _ = _norm_inputs(rows + dim, rows, dim, dtype, param, pad, offset)
+    out = _blank(rows, dim, dtype, pad, offset)
+    y, mean, rstd = features.layer_norm(x, w, b, out=out)
+    assert not pad or _gaps_untouched(out)
+    want = fo.layer_norm(x, w, b, float(torch.tensor(1e-5)), dtype)
+    for got, v, what in zip((y, mean, rstd), want, ("y", "mean", "rstd")):
+        _close(got, v, f"layer_norm {what}")
+
+
+def _check_norm_grad(rows, dim, dtype, param, pad=0, offset=0):
+    x, w, _, dy = _norm_inputs(rows + dim + 1, rows, dim, dtype, param, pad, offset)
+    _, mean, rstd = features.layer_norm(x)
+    out = _blank(rows, dim, dtype, pad, offset)
+    got = features.layer_norm_grad(dy, x, mean, rstd, w, out=out)
+    assert not pad or _gaps_untouched(out)
+    want = fo.layer_norm_grad(dy, x, mean, rstd, w, dtype, param)
+    for a, v, what in zip(got, want, ("x", "weight", "bias")):
+        _close(a, v, f"layer_norm_grad {what}")
+
+
+# At most 2,048 workgroups: these rows take two to three turns each, the last of them in part.  By width: elements one by
+# one, a part of a wave, a wave with one to four vectors a lane, 256 to 1,024 threads, and rows read three times.
+@pytest.mark.parametrize("dtype,param,rows,dim", [
+    (BF16, BF16, 150_001, 5), (F32, F32, 300_007, 3), (F32, F32, 300_007, 9), (F32, F32, 70_003, 40), (F32, F32, 20_005, 300), (F16, F32, 20_005, 700),
+    (BF16, F32, 20_005, 1_500), (F32, F32, 10_001, 1_000), (BF16, BF16, 9_001, 2_047), (F32, F32, 5_003, 1_500), (F32, F32, 4_500, 2_500),
+    (F16, F16, 5_000, 5_001), (F32, F32, 2_500, 5_001), (BF16, BF16, 2_500, 9_001), (F32, F32, 2_100, 7_001), (BF16, F32, 2_100, 17_001)])
+def test_layer_norm_turns(dtype, param, rows, dim):
+    _check_norm(rows, dim, dtype, param, pad=3, offset=1)
+
+
+# At most 512 workgroups, or 256 where a row takes 512 threads: two to three turns.
+@pytest.mark.parametrize("dtype,param,rows,dim", [
+    (BF16, BF16, 40_001, 5), (F32, F32, 80_001, 9), (F32, F32, 20_003, 40), (F32, F32, 5_003, 300), (F16, F32, 5_003, 700), (BF16, F32, 5_003, 1_500),
+    (F32, F32, 2_500, 1_000), (BF16, BF16, 1_300, 2_047), (F32, F32, 1_300, 1_500), (F32, F32, 600, 2_500), (BF16, F32, 600, 5_001),
+    (F32, F32, 520, 5_001), (BF16, BF16, 520, 9_001), (F32, F32, 520, 9_001), (BF16, BF16, 1_030, 17_001), (F32, F32, 1_030, 16_401)])
+def test_layer_norm_gradient_turns(dtype, param, rows, dim):
+    _check_norm_grad(rows, dim, dtype, param, pad=3, offset=1)
+
+
+# From 64 MB of output on, and from 288 MB of traffic in the backward pass, past the caches: odd widths at odd places.
+@pytest.mark.parametrize("dtype,param,rows,dim", [(F32, F32, 20_005, 901), (BF16, BF16, 40_001, 901), (F16, F32, 7_001, 5_001), (F32, F32, 1_100, 16_001),
+                                                  (BF16, F32, 4_200_001, 9), (F16, F16, 7_000_001, 5), (F32, F32, 14_001, 1_200), (BF16, BF16, 2_049, 16_383)])
+def test_layer_norm_past_the_caches(dtype, param, rows, dim):
+    assert rows * dim * dtype.itemsize >= 64 << 20
+    _check_norm(rows, dim, dtype, param, pad=1, offset=1)
+
+
+@pytest.mark.parametrize("dtype,param,rows,dim", [(F32, F32, 28_001, 901), (BF16, BF16, 56_003, 901), (F16, F32, 10_100, 5_001), (F32, F32, 2_800, 9_001),
+                                                  (BF16, F32, 5_700_001, 9), (F16, F16, 10_100_001, 5), (F32, F32, 21_001, 1_201), (BF16, BF16, 3_100, 16_383)])
+def test_layer_norm_gradient_past_the_caches(dtype, param, rows, dim):
+    assert rows * dim * 3 * dtype.itemsize >= 288 << 20
+    _check_norm_grad(rows, dim, dtype, param, pad=1, offset=1)
+
+
+# ---------------------------------------------------------------- clipping of many elements
+
+
+def _spread(g, dtype, lengths):
+    """Tensors at odd places of one buffer, with an element between each two."""
+    flat = (torch.randn(sum(lengths) + len(lengths) + 1, generator=g, device=DEV) * 0.01).to(dtype)
+    parts, at = [], 1
+    for n in lengths:
+        parts.append(flat[at:at + n])
+        at += n + 1
+    return flat, parts
+
+
+def _check_clip(dtype, to, lengths, limit):
+    _, grads = _spread(_on_gpu(len(lengths) + lengths[0]), dtype, lengths)
+    room = _nan(sum(lengths) + 2 * len(lengths), dtype=to)
+    outs, at, gaps = [], 1, [0]
+    for n in lengths:
+        outs.append(room[at:at + n])
+        gaps.append(at + n)
+        at += n + 1
+    norm = features.clip_grads(grads, limit, out=outs)
+    want_norm, want = fo.clip(grads, float(torch.tensor(limit)), [to] * len(grads))
+    _close(norm, want_norm, "norm")
+    assert torch.equal(features.grad_norm(grads), norm)
+    for i, (o, v) in enumerate(zip(outs, want)):
+        _close(o, v, f"clip {i}")
+    assert torch.isnan(room[torch.tensor(gaps, device=DEV)]).all()
+    if to == dtype:
+        features.clip_grads(grads, limit)
+        assert all(torch.equal(a, b) for a, b in zip(grads, outs))
+
+
+# From 4,194,304 elements on, chunks are 8,192 elements and whole ones are read at once.
+@pytest.mark.parametrize("limit", [1.0, 1e6])
+@pytest.mark.parametrize("dtype,to", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+def test_clip_whole_chunks(dtype, to, limit):
+    _check_clip(dtype, to, [8_191, 8_192, 8_193, 3_000_001, 5, 1_300_000, 16_384, 1], limit)
+
+
+# Beyond 224 MB the first kernel reads past the caches what the second cannot find there: within a launch of up to 100
+# tensors, and over several.
+@pytest.mark.parametrize("dtype,to,lengths", [(BF16, F32, [70_000_001, 8_192, 60_000_000, 77]), (F32, F32, [33, 40_000_001, 30_000_003]),
+                                              (F16, F16, [130_000_001]), (F32, F32, [300_001 + 7 * k for k in range(230)])])
+def test_clip_more_than_the_caches_hold(dtype, to, lengths):
+    assert sum(lengths) * dtype.itemsize > 224 << 20
+    _check_clip(dtype, to, lengths, 1.0)
 
 
 # ---------------------------------------------------------------- beside autograd
