@@ -15,6 +15,8 @@ from paper_1702_07005_amd import features  # noqa: E402
 
 DEV = "cuda"
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+PAIRS = [(a, b) for a in (F32, BF16, F16) for b in (F32, BF16, F16)]
+NORM_PAIRS = [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)]
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -107,6 +109,25 @@ def test_embed_past_the_caches(table, to, n, rows, dim):
     fo.close(out[:2000], fo.embed(t[:2000].cpu(), e.cpu(), float(torch.tensor(1.3)), to), "embed")
 
 
+# The pairs of element types, both kinds of ids, rows narrower than a vector and wider ones: one row in flight, four, and
+# four past the caches (in pieces of it four, bit for bit the same).
+@pytest.mark.parametrize("ids", [torch.int32, torch.int64])
+@pytest.mark.parametrize("table,to", PAIRS)
+@pytest.mark.parametrize("dim", [3, 37])
+def test_embed_types(dim, table, to, ids):
+    g = _on_gpu(dim)
+    rows = 1_001
+    e = _matrix(g, rows, dim, table, pad=2, offset=1)
+    n = (96 << 20) // (dim * to.itemsize) + 1
+    t = torch.randint(-2, rows + 2, (n,), generator=g, device=DEV).to(ids)
+    out = features.embed(t, e, scale=1.3, out=_blank(n, dim, to, 1, 1))
+    assert _gaps_untouched(out)
+    for at, k in ((0, 300), (0, n // 4), (n - n // 4, n // 4)):
+        part = features.embed(t[at:at + k], e, scale=1.3, dtype=to)
+        assert torch.equal(torch.isnan(part), torch.isnan(out[at:at + k])) and torch.equal(part.nan_to_num(), out[at:at + k].nan_to_num())
+    fo.close(out[:5_000], fo.embed(t[:5_000].cpu(), e.cpu(), float(torch.tensor(1.3)), to), "embed")
+
+
 # ---------------------------------------------------------------- zeros of the lookup gradient
 
 
@@ -187,6 +208,32 @@ def test_embed_grad_long_runs(n, rows, dim, width):
     assert torch.equal(out, again)
 
 
+# The pairs of element types with both kinds of ids and accumulation: a single launch, and the sums in workgroups of 256
+# and 512 threads; rows narrower than a vector, and wider ones.
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("grad,to", PAIRS)
+@pytest.mark.parametrize("n,rows,dim", [(900, 200, 3), (900, 200, 37), (2_001, 200, 3), (2_001, 200, 37), (2_001, 200, 515)])
+def test_embed_grad_types(n, rows, dim, grad, to, accumulate):
+    g = _gen(n + dim)
+    t = _tokens(g, n, rows, "zipf")
+    d = _gradients(g, t, rows, dim, grad)
+    before = torch.randn(rows, dim, generator=g).to(to) if accumulate else None
+    want = fo.embed_grad(t, d, rows, 0.75, to, before)
+    for ids in (torch.int32, torch.int64):
+        out = before.to(DEV) if accumulate else _nan(rows, dim, dtype=to)
+        features.embed_grad(t.to(DEV, ids), d.to(DEV), rows, scale=0.75, out=out, accumulate=accumulate)
+        fo.close(out, want, "embed_grad")
+
+
+@pytest.mark.parametrize("n", [30_000, 40_000, 300_000, 900_000])
+def test_embed_grad_sorts_of_narrow_ids(n):
+    g = _gen(n)
+    t = _tokens(g, n, 50_001, "zipf")
+    d = _gradients(g, t, 50_001, 4, F32)
+    wide = features.embed_grad(t.to(DEV), d.to(DEV), 50_001)
+    assert torch.equal(features.embed_grad(t.int().to(DEV), d.to(DEV), 50_001, out=_nan(50_001, 4)), wide)
+
+
 @pytest.mark.parametrize("n", [3_000, 70_000])
 def test_embed_grad_of_one_gradient_for_all_tokens(n):
     g = _gen(n)
@@ -262,6 +309,25 @@ def test_layer_norm_past_the_caches(dtype, param, rows, dim):
 def test_layer_norm_gradient_past_the_caches(dtype, param, rows, dim):
     assert rows * dim * 3 * dtype.itemsize >= 288 << 20
     _check_norm_grad(rows, dim, dtype, param, pad=1, offset=1)
+
+
+# Every width of a row's group of lanes, one less than the vectors that fill it (2,045 columns: 512 vectors of fp32, 256 of
+# 16 bits), within the caches and past them.
+WIDTHS = [3, 13, 29, 61, 125, 253, 509, 765, 1_021, 1_533, 2_045, 4_093, 8_189, 16_381]
+
+
+@pytest.mark.parametrize("dtype,param", NORM_PAIRS)
+@pytest.mark.parametrize("dim", WIDTHS)
+def test_layer_norm_widths(dim, dtype, param):
+    _check_norm(41, dim, dtype, param, pad=1, offset=1)
+    _check_norm((64 << 20) // (dim * dtype.itemsize) + 1, dim, dtype, param, pad=1, offset=1)
+
+
+@pytest.mark.parametrize("dtype,param", NORM_PAIRS)
+@pytest.mark.parametrize("dim", WIDTHS)
+def test_layer_norm_gradient_widths(dim, dtype, param):
+    _check_norm_grad(41, dim, dtype, param, pad=1, offset=1)
+    _check_norm_grad((288 << 20) // (3 * dim * dtype.itemsize) + 1, dim, dtype, param, pad=1, offset=1)
 
 
 # ---------------------------------------------------------------- clipping of many elements
