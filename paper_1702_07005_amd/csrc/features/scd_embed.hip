@@ -1081,10 +1081,12 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
             k_sums<VEC, ACC, THREADS><<<grid, THREADS, 0, s>>>(a, (const TG*)grad, (TO*)out, m.log2_lanes);
             if (blocks > 1) k_sums_join<VEC, ACC, THREADS><<<join, THREADS, 0, s>>>(a, (TO*)out, m.log2_lanes);
         };
-        if (sums_threads(m) == kWideSums)
-            accumulate ? go(std::true_type{}, Int<kWideSums>{}) : go(std::false_type{}, Int<kWideSums>{});
-        else
-            accumulate ? go(std::true_type{}, Int<kThreads>{}) : go(std::false_type{}, Int<kThreads>{});
+        if constexpr (VEC > 1)  // a row without whole vectors is narrow
+            if (sums_threads(m) == kWideSums) {
+                accumulate ? go(std::true_type{}, Int<kWideSums>{}) : go(std::false_type{}, Int<kWideSums>{});
+                return;
+            }
+        accumulate ? go(std::true_type{}, Int<kThreads>{}) : go(std::false_type{}, Int<kThreads>{});
     });
     return launched("scd_embed_grad");
 }
