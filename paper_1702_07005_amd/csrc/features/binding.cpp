@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <algorithm>
 #include <string>
 #include <vector>
 
@@ -290,6 +291,33 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Refuses a tensor that is written to and shares memory with another one of the call, whose elements would be scaled twice
+// or read after the write.  A span that is clipped in place is one range.
+void check_apart(const std::vector<scd_span_t>& spans) {
+    struct Range {
+        uintptr_t from, to;
+        bool written;
+    };
+    const auto bytes = [](int64_t n, int32_t type) { return (uintptr_t)n * (type == SCD_F32 ? 4 : 2); };
+    std::vector<Range> ranges;
+    ranges.reserve(2 * spans.size());
+    bool writes = false;
+    for (const scd_span_t& s : spans) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(s.src), q = reinterpret_cast<uintptr_t>(s.dst);
+        if (s.n == 0) continue;
+        if (p != q) ranges.push_back(Range{p, p + bytes(s.n, s.src_type), false});
+        if (q) ranges.push_back(Range{q, q + bytes(s.n, s.dst_type), true});
+        writes |= q != 0;
+    }
+    if (!writes || ranges.size() < 2) return;
+    std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t read = 0, written = 0;  // where the ranges before end
+    for (const Range& r : ranges) {
+        if (r.from < written || (r.written && r.from < read)) refuse("a tensor that is written to shares memory with another one of the call");
+        (r.written ? written : read) = std::max(r.written ? written : read, r.to);
+    }
+}
+
 // clip(device, stream, grads, outs, max_norm): outs is grads for clipping in place, None for the norm alone.
 PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -325,6 +353,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
         check_writable(o, "output " + std::to_string(i));
         s.dst = o.data_ptr();
     }
+    check_apart(spans);
     if (device.index() != c.device) return none();
     int64_t need = 0;
     check(scd_clip_grads_workspace(&need));

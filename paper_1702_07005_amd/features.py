@@ -113,7 +113,8 @@ def clip_grads(grads, max_norm, out=None, stream=None):
     tensors of ``out`` (each of its gradient's type or float32).  Returns the norm before, a float32 tensor on
     the GPU, without waiting for it.
 
-    The tensors are contiguous, of float32, bfloat16 or float16, and on one device."""
+    The tensors are contiguous, of float32, bfloat16 or float16, and on one device.  Those that are written to share no
+    memory with others of the call."""
     grads = grads if isinstance(grads, (list, tuple)) else list(grads)
     return _clip(grads, grads if out is None else out, max_norm, stream)
 

@@ -379,6 +379,22 @@ def test_clip_more_than_the_caches_hold(dtype, to, lengths):
     _check_clip(dtype, to, lengths, 1.0)
 
 
+def test_clip_refuses_shared_memory():
+    x, o = torch.randn(100, device=DEV), torch.randn(100, device=DEV)
+    empty = x[:0]
+    for grads, outs in (([x, x], None), ([x[:60], o, x[59:]], None), ([x[:60]], [x[1:61]]), ([x, o], [o, x]), ([x[:50], x[50:]], [o[:50], o[:50]]),
+                        ([x[:50], x[50:]], [x[:50], x[49:99]]), ([x, x], [x, o])):
+        before = x.clone(), o.clone()
+        with pytest.raises(ValueError, match="shares memory"):
+            features.clip_grads(grads, 1e-3, out=outs)
+        assert torch.equal(x, before[0]) and torch.equal(o, before[1])
+    twice = features.grad_norm([x, x])
+    assert abs(float(twice) / float(features.grad_norm([x])) - 2 ** 0.5) < 1e-6
+    features.clip_grads([x, x], 1e-3, out=[o, torch.empty_like(o)])
+    features.clip_grads([x[50:], empty, x[:50], x[50:50]], 1e-3)
+    features.clip_grads([x[:50], x[50:]], 1e-3, out=[x[:50], o[:50]])
+
+
 # ---------------------------------------------------------------- beside autograd
 
 
