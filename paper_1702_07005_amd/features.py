@@ -9,7 +9,8 @@ graphs.  There is no fallback: if the binding is not built this module raises on
 
 Matrices may be views with any row stride, but their last dimension has unit stride.  Work is enqueued on
 the current stream, or on ``stream`` (a torch stream or a raw handle), with which the caller orders the
-inputs; outputs that the call allocates then belong to that stream.
+inputs; outputs that the call allocates then belong to that stream, and the other tensors may be dropped once the call
+returns.
 
 The operators are outside autograd: they record nothing, results never require gradients, and backward passes are
 calls of their own.  Tensors that a call writes to (``out``, gradients clipped in place) count it as an in-place
@@ -39,7 +40,8 @@ _stream = torch._C._cuda_getCurrentRawStream
 
 
 def _elsewhere(tensor, stream, call, *args):
-    """Makes the call on the tensor's device, or on a given stream, by making that the current one."""
+    """Makes the call on the tensor's device, or on a given stream, by making that the current one.  The memory of tensors
+    that belong to another stream is not given away before the given one is done with them."""
     if not (isinstance(tensor, torch.Tensor) and tensor.is_cuda):
         raise ValueError("CUDA tensors are needed")
     if stream is None:
@@ -50,6 +52,10 @@ def _elsewhere(tensor, stream, call, *args):
         if stream.device != tensor.device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {tensor.device}")
         context = torch.cuda.stream(stream)
+        for a in args:
+            for t in a if isinstance(a, (list, tuple)) else (a,):
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
     with context:
         return call(*args)
 

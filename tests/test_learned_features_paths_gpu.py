@@ -395,6 +395,44 @@ def test_clip_refuses_shared_memory():
     features.clip_grads([x[:50], x[50:]], 1e-3, out=[x[:50], o[:50]])
 
 
+# ---------------------------------------------------------------- streams
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_inputs_may_be_dropped_while_another_stream_reads_them(raw):
+    n, rows, dim = 20_000, 700, 64
+    g = _gen(5)
+    ids = torch.randint(0, rows, (n,), generator=g)
+    x, table = torch.randn(n, dim, generator=g), torch.randn(rows, dim, generator=g)
+    main, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+
+    def held(call, *inputs):
+        """A call on the other stream, which nothing but the call holds the inputs of."""
+        main.synchronize()  # they are made
+        return call(*inputs, stream=stream)
+
+    def calls():
+        d, t, e = x.to(DEV), ids.to(DEV), table.to(DEV)
+        y, mean, rstd = features.layer_norm(d)
+        dx, _, _ = features.layer_norm_grad(y, d, mean, rstd)
+        yield features.embed(t, e), lambda: held(features.embed, t.clone(), e.clone())
+        yield features.embed_grad(t, d, rows), lambda: held(lambda t, d, stream: features.embed_grad(t, d, rows, stream=stream), t.clone(), d.clone())
+        yield y, lambda: held(features.layer_norm, d.clone())[0]
+        yield dx, lambda: held(features.layer_norm_grad, y.clone(), d.clone(), mean.clone(), rstd.clone())[0]
+        yield features.grad_norm([d, e]), lambda: held(lambda d, e, stream: features.grad_norm([d, e], stream=stream), d.clone(), e.clone())
+
+    for k, (want, call) in enumerate(calls()):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)  # the call's work waits behind this
+        got = call()
+        spoil = [torch.full((m,), float("nan"), device=DEV) for m in (n * dim, n * dim, rows * dim, 2 * n, n, n)]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), k
+        del spoil
+
+
 # ---------------------------------------------------------------- beside autograd
 
 
