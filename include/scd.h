@@ -432,8 +432,9 @@ typedef struct {
 /* Clips `count` >= 0 tensors together by their norm: norm = sqrt(sum of the squares of all elements), factor =
  * max_norm / norm if norm > max_norm, else 1; dst = factor * src for every span.  Where dst is src, a factor of
  * 1 writes nothing; a span whose dst is NULL only counts towards the norm.  Squares are summed in 64 bits, so no
- * finite input overflows.  A NaN makes norm and factor NaN, an infinity makes norm infinite and factor 0, so
- * that both show in what is written (with max_norm = infinity the factor of an infinite norm is 1).
+ * finite input overflows (*norm_dev is infinite where the norm is beyond float32; the factor comes from the 64-bit
+ * one).  A NaN makes norm and factor NaN, an infinity makes norm infinite and factor 0, so that both show in what
+ * is written (with max_norm = infinity the factor of an infinite norm is 1).
  *   spans: host array (read before the call returns);  max_norm >= 0 (infinity: the norm alone is of interest);
  *   norm_dev: float32[1], device;  workspace_dev: scd_clip_grads_workspace bytes (16-byte aligned, device). */
 int scd_clip_grads_workspace(int64_t *bytes);

@@ -28,6 +28,9 @@ namespace {
 // A large output goes past the caches (ONCE), so that the table's rows stay there.  2.6 M ids into 1.5 M x 16 (fp32, 164 MB
 // out): 63 us through the caches, 53 past them; 16,384 x 4,096 (bf16, 134 MB): 42 and 34, and with the layer norm that
 // reads them 88 and 86; but 4,096 x 4,096 (34 MB), which the norm then finds in the caches: 22.8 and 25.7 together.
+// On both sides of the limit, alone and with a pass that reads the output at once: 80 MB of rows of 16 (fp32) 34 through
+// and 24 past the caches, 50 and 53; 112 MB 47 and 33, 69 and 71.  The reader's loss falls from 8 % to 3 %, the lookup's gain
+// stays.
 constexpr int64_t kOnceBytes = int64_t(96) << 20;
 
 template <int VEC, int U, bool ONCE, typename TI, typename TT, typename TO>
@@ -726,8 +729,10 @@ __global__ void __launch_bounds__(THREADS) k_sums_join(SumArgs a, TO* __restrict
 // With at most kFewMax tokens one launch does it all: a workgroup owns some consecutive rows (and, of wide ones, a column
 // range), picks the tokens that lie in them, orders them by counting, fills the other rows with zeros and sums the runs,
 // long ones with several groups.  Every workgroup reads all tokens, so this is for lists that cost less than
-// the launches of a sort.
+// the launches of a sort.  1,024 tokens, one to each thread, are where it ends: they still take less than by the sort
+// (75,000 x 1,024 in bf16 32 and 39 us, 1.5 M x 16 in fp32 19 and 27, 1,000 x 64 in fp32 10 and 16).
 constexpr int kFewThreads = 1024;
+static_assert(kFewMax <= kFewThreads, "a thread holds a token");
 constexpr int kFewRows = 16384;  // of a workgroup at most: a bit each in LDS
 constexpr int64_t kFlatBytes = int64_t(64) << 20;
 
@@ -1011,7 +1016,10 @@ extern "C" int scd_embed_grad(const void* tokens, int32_t token_type, int64_t n,
             const int64_t own = std::min<int64_t>(kFewRows, std::max(least, ceil_div(rows * m.ranges, 512)));
             const dim3 grid((uint32_t)ceil_div(rows, own), m.ranges);
             // A large table without gaps between its rows: 3 tokens into 75,829 x 1,055 (fp32) 95 us by rows, 75 by pieces;
-            // 300 into 4,999 x 777 8.7 and 10.6.
+            // 300 into 4,999 x 777 8.7 and 10.6.  Pieces gain where rows come in ranges that end inside a line, and lose time
+            // to many tokens: 3, 300 and 1,000 tokens into 1,055 columns 11.0, 13.7 and 16.0 us by rows and 10.2, 15.4 and
+            // 22.0 by pieces at 32 MB, 14.5, 17.2, 19.9 and 12.5, 17.1, 23.8 at 64 MB, 20.9, 24.0, 27.3 and 18.1, 20.8, 27.0
+            // at 96 MB; 777 columns at 64 MB 12.6, 14.5, 16.6 and 13.1, 15.9, 18.7, at 320 MB 85, 86, 88 and 76, 80, 85.
             a.flat = a.ostride == dim && rows * dim * (int64_t)sizeof(TO) >= kFlatBytes;
             const auto go = [&](auto ti, auto acc) {
                 using TI = decltype(ti);

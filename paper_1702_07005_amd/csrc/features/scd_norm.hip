@@ -82,6 +82,9 @@ struct NormArgs {
 
 // A large output goes past the caches (ONCE): 100,000 x 624 (fp32, 250 MB out) 98.4 us through them, 95.5 past them,
 // 16,384 x 2,048 (bf16, 67 MB) 25.3 and 22.4; a smaller one is left there for its reader.
+// With a pass that reads the output at once, both together take 4 to 10 % less through the caches at every size up to
+// 256 MB: 12,288 x 2,048 (50 MB) 20.9 through and 17.8 past them alone, 35.6 and 38.5 with the reader, 24,576 x 2,048
+// (101 MB) 38.2 and 35.8, 62.7 and 69.4.
 constexpr int64_t kOnceOut = int64_t(64) << 20;
 
 template <int VEC, int NV, int LPR, int THREADS, bool ONCE, typename T, typename P>
@@ -156,7 +159,9 @@ __global__ void __launch_bounds__(THREADS) k_norm(NormArgs<T, P> a) {
     }
 }
 
-// Rows too wide for the registers: a workgroup reads its row three times (from the caches after the first).
+// Rows too wide for the registers: a workgroup reads its row three times (from the caches after the first), element by
+// element, which bounds it: 4,096 x 32,768 forward 458 us in bf16 (1.2 TB/s) and 404 in fp32 (2.7 TB/s); backward, where dw
+// and db go through the workspace with every row, 800 (1.0 TB/s) and 990 (1.6 TB/s).
 constexpr int kWideThreads = 1024;
 
 template <typename T, typename P>
@@ -211,6 +216,9 @@ struct NormGradArgs {
 // Where the three matrices take more than the caches hold (ONCE), they are read and written past them: 50,000 x 624
 // (fp32, 374 MB) 71.8 us through the caches, 66.3 past them, 16,384 x 4,096 (bf16, 403 MB) 79.5 and 76.5; but
 // 4,096 x 4,096 (101 MB), whose inputs the caches may hold, 24.8 and 30.4.
+// On both sides of the limit: 10,922 x 4,096 (bf16, 268 MB) 57.5 and 55.8, 13,653 x 4,096 (336 MB) 68.6 and 66.3;
+// 35,848 x 624 (fp32, 268 MB) 53.1 and 49.4, 44,810 x 624 (336 MB) 64.6 and 59.8; with a pass that reads dx at once 80 and
+// 84, 98 and 101 (bf16), 70.8 and 70.5, 85.8 and 85.4 (fp32).
 constexpr int64_t kOnceBytes = int64_t(288) << 20;
 
 template <int VEC, int NV, int LPR, int THREADS, bool ONCE, typename T, typename P>

@@ -133,8 +133,8 @@ def test_embed_grad_types(grad, out, n, rows, dim):
     fo.close(got, fo.embed_grad(t, d, rows, 1.5, TYPES[out]), "embed_grad")
 
 
-# Around the sorts' limits: a wave, one workgroup with 1, 4 and 16 keys a thread, and tiles of 4,096 in one, two and
-# three passes.
+# Around the sorts' limits: one launch up to 1,024 tokens, tiles up to 16,384 or, where a key has several digits, 32,768,
+# and the radix sort with two entries a thread in one and two passes.
 @pytest.mark.parametrize("kind", ["even", "zipf", "one", "none", "outside"])
 @pytest.mark.parametrize("n,rows,dim", [(64, 3, 16), (1023, 300, 5), (1024, 70_000, 8), (1025, 513, 8), (4096, 511, 9), (4097, 512, 4),
                                         (16_384, 1025, 8), (16_385, 7, 8), (16_390, 2047, 6), (40_001, 2048, 8), (50_000, 300_000, 3),
@@ -489,7 +489,7 @@ def test_refusals():
             f()
 
 
-# Few tokens take one launch without a sort; around its limit of 512, with long runs, wide rows and more rows than one
+# Few tokens take one launch without a sort, up to 1,024 of them; with long runs, wide rows and more rows than one
 # workgroup's 16,384.
 @pytest.mark.parametrize("kind", ["even", "zipf", "one", "none", "outside"])
 @pytest.mark.parametrize("n,rows,dim", [(2, 40_000, 3), (64, 20, 40), (300, 17_000_000, 1), (511, 33, 2050), (512, 700, 130), (513, 700, 130)])
