@@ -362,7 +362,9 @@ int scd_objective_static(const scd_matrix_t *A, const float *y_dev, double lambd
  * Operators for models whose coordinates are not one-hot columns but rows of a learned table: ids are
  * looked up (scd_embed), the vectors normalised (scd_layer_norm), a read-out is fitted on them by the
  * solver above, and the table is trained by the read-out's gradient, which goes back through both
- * (scd_layer_norm_grad, scd_embed_grad) and is clipped by its global norm (scd_clip_grads).
+ * (scd_layer_norm_grad, scd_embed_grad), is clipped by its global norm (scd_clip_grads), and moves the table
+ * (scd_adamw).  scd_rms_norm and scd_rms_norm_grad take the place of the layer norm in models that normalise by the
+ * root mean square.
  *
  * Conventions of these calls:
  *   - They take no handle, keep nothing between calls, enqueue on `stream` only and never synchronise;
@@ -376,7 +378,7 @@ int scd_objective_static(const scd_matrix_t *A, const float *y_dev, double lambd
  *   - Results are bit-identical from call to call: no sum depends on the order in which waves run.
  * Errors: SCD_ERR_INVALID (null pointer, size, stride, unaligned workspace), SCD_ERR_UNSUPPORTED (a
  * type, or a pair of types, that the call does not take), SCD_ERR_HIP. */
-typedef enum { SCD_F32 = 0, SCD_BF16 = 1, SCD_F16 = 2, SCD_I32 = 3, SCD_I64 = 4 } scd_type_t;
+typedef enum { SCD_F32 = 0, SCD_BF16 = 1, SCD_F16 = 2, SCD_I32 = 3, SCD_I64 = 4, SCD_E4M3 = 5 } scd_type_t;
 
 /* out[t, :] = scale * table[tokens[t], :], t < n.  A negative token is a padded place and gives zeros; a
  * token of at least `rows` names no row and gives NaN.
@@ -440,6 +442,91 @@ typedef struct {
 int scd_clip_grads_workspace(int64_t *bytes);
 int scd_clip_grads(const scd_span_t *spans, int64_t count, float max_norm, float *norm_dev, void *workspace_dev,
                    int64_t workspace_bytes, void *stream);
+
+/* y[r, :] = h * rstd[r] * weight, rstd = 1/sqrt(mean of h^2 + eps) over the row, h = x, or with a residual h = x +
+ * residual rounded to `type`, which is written to sum: the norm is of the rounded values, and scd_rms_norm_grad takes
+ * them.
+ *   x_dev, residual_dev (NULL: none), sum_dev (not NULL with a residual, unused without): [rows, dim] of `type`;
+ *   weight_dev: [dim] of param_type (`type` or SCD_F32) or NULL (1);  rstd_dev: float32[rows], NULL to leave it out;
+ *   eps >= 0.  y_dev: [rows, dim] of y_type, which is `type` or SCD_E4M3.
+ * With SCD_E4M3 (8 bits: 4 of exponent, 3 of mantissa, 448 at most, no infinity) y is divided by its scale and rounded
+ * once, to the nearest, ties to even; scale = max(largest |y| / 448, 2^-126).  group = 0: one scale for each row, scale_dev:
+ * float32[rows];  group = 32, 64 or 128: one for each `group` columns (the last group may be shorter), scale_dev:
+ * float32[rows, ceil(dim / group)].  A NaN gives NaN and does not count for the scale; an infinite y makes its scale
+ * infinite and itself NaN.  Otherwise group is 0 and scale_dev is unused.
+ * y may be x or residual unless it has 8 bits, and sum may be x or residual, with the same stride; y is not sum.  Squares
+ * are summed in 32 bits: rows whose mean square is beyond float32 give zeros. */
+int scd_rms_norm(const void *x_dev, int32_t type, int64_t x_stride, const void *residual_dev, int64_t residual_stride,
+                 int64_t rows, int64_t dim, const void *weight_dev, int32_t param_type, float eps, void *y_dev,
+                 int32_t y_type, int64_t y_stride, float *scale_dev, int64_t group, void *sum_dev, int64_t sum_stride,
+                 float *rstd_dev, void *stream);
+
+/* The gradients of scd_rms_norm (before a rounding to 8 bits) with respect to h and weight.  With n = h * rstd and g =
+ * grad * weight, all over the row:
+ *   dh = rstd * (g - n * mean(g * n)) + residual_grad;   dweight = sum over rows of grad * n.
+ * dh is the gradient of x and of the residual alike; residual_grad_dev (NULL: none) is what reaches h another way.
+ *   grad_dev, h_dev, residual_grad_dev, dh_dev: [rows, dim] of `type` (dh may be any of the inputs, with its stride);
+ *   rstd_dev: float32[rows] as scd_rms_norm wrote them;  weight_dev: [dim] of param_type or NULL (1);  dweight_dev:
+ *   [dim] of param_type, NULL to leave it out.
+ * scd_rms_norm_grad_workspace: bytes of scratch (16-byte aligned, device), 0 where dweight is NULL. */
+int scd_rms_norm_grad_workspace(int64_t rows, int64_t dim, int64_t *bytes);
+int scd_rms_norm_grad(const void *grad_dev, int64_t grad_stride, const void *h_dev, int64_t h_stride, int32_t type,
+                      const float *rstd_dev, int64_t rows, int64_t dim, const void *weight_dev, int32_t param_type,
+                      const void *residual_grad_dev, int64_t residual_stride, void *dh_dev, int64_t dh_stride,
+                      void *dweight_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* One tensor of scd_adamw: n elements of each.
+ *   param: of param_type;  grad: of grad_type (any with SCD_F32 parameters; otherwise param_type or SCD_F32);
+ *   copy: NULL, or of copy_type (SCD_BF16 or SCD_F16, with SCD_F32 parameters): the new parameters, rounded;
+ *   state_type SCD_F32: m, v: float32[n], m_scale and v_scale unused;
+ *   state_type SCD_E4M3: m, v: 8 bits [n], m_scale, v_scale: float32[ceil(n / 256)], one for each 256 consecutive
+ *   elements (the last block may be shorter).  m holds m / m_scale, v holds sqrt(v) / v_scale.
+ * All zeros is the state before the first step.  What is written overlaps nothing else of the call. */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m;
+    void *v;
+    float *m_scale;
+    float *v_scale;
+    void *copy;
+    int64_t n;
+    float weight_decay; /* >= 0 */
+    int32_t param_type;
+    int32_t grad_type;
+    int32_t state_type;
+    int32_t copy_type;
+} scd_adamw_span_t;
+
+/* What the tensors of scd_adamw share.  lr_dev, step_dev and norm_dev are device scalars, or NULL; they are read when the
+ * call runs, so that a captured call follows them. */
+typedef struct {
+    double lr;               /* >= 0; unused with lr_dev */
+    double beta1;            /* in [0, 1) */
+    double beta2;            /* in [0, 1) */
+    double eps;              /* >= 0 */
+    int64_t step;            /* the number of this step, from 1; unused with step_dev */
+    const float *lr_dev;
+    const int64_t *step_dev; /* a value below 1 counts as 1 */
+    const float *norm_dev;   /* of all gradients together, as scd_clip_grads gives it */
+    float max_norm;          /* >= 0; unused without norm_dev */
+    uint32_t seed;           /* of the rounding of states of 8 bits */
+} scd_adamw_t;
+
+/* One AdamW step over `count` >= 0 tensors, t = step:
+ *   g = f * grad, f = max_norm / norm if norm > max_norm, else 1;   m = beta1 m + (1 - beta1) g;
+ *   v = beta2 v + (1 - beta2) g^2;
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * Parameters move by m and v in 32 bits, before these are rounded; a NaN norm makes f NaN, an infinite one 0, as in
+ * scd_clip_grads, so that with norm_dev the gradients need not be written clipped.
+ * States of 8 bits: the scales are max(largest / 448, 2^-126) of the block's finite |m| and sqrt(v), others become NaN; m / m_scale goes
+ * to one of its neighbours in 8 bits with probabilities that keep its mean, sqrt(v) / v_scale with those that keep the
+ * mean of its square, but away from 0.  With fmix32 the finaliser of MurmurHash3, element i of the k-th tensor takes
+ *   word = fmix32(low 32 bits of i xor (fmix32(fmix32(seed xor fmix32(low 32 bits of t)) + k) + high 32 bits of i)),
+ * and goes away from 0 where (word mod 2^16 + 1/2) / 2^16 (m), (word / 2^16 + 1/2) / 2^16 (sqrt(v); word / 2^16 without
+ * its fraction) is less than the probability of that.
+ *   spans, options: host memory (read before the call returns). */
+int scd_adamw(const scd_adamw_span_t *spans, int64_t count, const scd_adamw_t *options, void *stream);
 
 /* Message describing the last error on the calling thread ("" if none). */
 const char *scd_last_error(void);

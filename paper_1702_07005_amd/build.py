@@ -24,7 +24,7 @@ PROBE_LIB = os.path.join(HERE, "libscdprobe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "ceiling.hip")]
 
 # The operators of learned features: kernels of the same library, which no solver call runs.
-FEATURE_SOURCES = [os.path.join(CSRC, "features", f) for f in ("scd_embed.hip", "scd_norm.hip", "scd_clip.hip")]
+FEATURE_SOURCES = [os.path.join(CSRC, "features", f) for f in ("scd_embed.hip", "scd_norm.hip", "scd_rms.hip", "scd_clip.hip", "scd_adamw.hip")]
 # Their binding: host code against torch's C++ headers and libscd.
 BINDING = os.path.join(HERE, "_features.so")
 BINDING_SOURCE = os.path.join(CSRC, "features", "binding.cpp")

@@ -56,11 +56,12 @@ struct Call {
         if (v == -1 && PyErr_Occurred()) throw python_error();
         return v;
     }
-    static float real(PyObject* o) {
+    static double real64(PyObject* o) {
         const double v = PyFloat_AsDouble(o);
         if (v == -1.0 && PyErr_Occurred()) throw python_error();
-        return (float)v;
+        return v;
     }
+    static float real(PyObject* o) { return (float)real64(o); }
     // The k-th argument: a tensor, which lives as long as the call.
     const at::Tensor& tensor(int k, const char* what) const {
         if (!THPVariable_Check(args[k])) refuse(std::string(what) + " must be a tensor");
@@ -86,11 +87,12 @@ struct Rows {
     int32_t type;
 };
 
-Rows rows_of(const at::Tensor& t, const char* what) {
-    const int32_t type = element(t.scalar_type());
+// `eight`: of 8 bits (e4m3).
+Rows rows_of(const at::Tensor& t, const char* what, bool eight = false) {
+    const int32_t type = eight ? t.scalar_type() == at::kFloat8_e4m3fn ? SCD_E4M3 : -1 : element(t.scalar_type());
     const int64_t d = t.dim();
     if (type < 0 || !t.is_cuda() || d < 1)
-        refuse(std::string(what) + " must be a CUDA tensor of float32, bfloat16 or float16 with at least one dimension");
+        refuse(std::string(what) + " must be a CUDA tensor of " + (eight ? "float8_e4m3fn" : "float32, bfloat16 or float16") + " with at least one dimension");
     const auto sizes = t.sizes(), strides = t.strides();
     Rows r{t.data_ptr(), 1, sizes[d - 1], sizes[d - 1], type};
     for (int64_t i = 0; i < d - 1; ++i) r.n *= sizes[i];
@@ -291,31 +293,45 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// Refuses a tensor that is written to and shares memory with another one of the call, whose elements would be scaled twice
-// or read after the write.  A span that is clipped in place is one range.
-void check_apart(const std::vector<scd_span_t>& spans) {
-    struct Range {
-        uintptr_t from, to;
-        bool written;
-    };
-    const auto bytes = [](int64_t n, int32_t type) { return (uintptr_t)n * (type == SCD_F32 ? 4 : 2); };
-    std::vector<Range> ranges;
-    ranges.reserve(2 * spans.size());
+// A range of memory that a call over many tensors reads or writes.
+struct Range {
+    uintptr_t from, to;
+    bool written;
+};
+
+struct Ranges {
+    std::vector<Range> all;
     bool writes = false;
+    void add(const void* p, int64_t bytes, bool written) {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+        if (bytes == 0) return;
+        all.push_back(Range{from, from + (uintptr_t)bytes, written});
+        writes |= written;
+    }
+    void add(const at::Tensor& t, bool written) { add(t.data_ptr(), (int64_t)t.nbytes(), written); }
+    // Refuses a tensor that is written to and shares memory with another one of the call, whose elements would be written
+    // twice or read after the write.
+    void check_apart() {
+        if (!writes || all.size() < 2) return;
+        std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+        uintptr_t read = 0, written = 0;  // where the ranges before end
+        for (const Range& r : all) {
+            if (r.from < written || (r.written && r.from < read)) refuse("a tensor that is written to shares memory with another one of the call");
+            (r.written ? written : read) = std::max(r.written ? written : read, r.to);
+        }
+    }
+};
+
+// A span that is clipped in place is one range.
+void check_apart(const std::vector<scd_span_t>& spans) {
+    const auto bytes = [](int64_t n, int32_t type) { return n * (type == SCD_F32 ? 4 : 2); };
+    Ranges ranges;
+    ranges.all.reserve(2 * spans.size());
     for (const scd_span_t& s : spans) {
-        const uintptr_t p = reinterpret_cast<uintptr_t>(s.src), q = reinterpret_cast<uintptr_t>(s.dst);
-        if (s.n == 0) continue;
-        if (p != q) ranges.push_back(Range{p, p + bytes(s.n, s.src_type), false});
-        if (q) ranges.push_back(Range{q, q + bytes(s.n, s.dst_type), true});
-        writes |= q != 0;
+        if (s.src != s.dst) ranges.add(s.src, bytes(s.n, s.src_type), false);
+        if (s.dst) ranges.add(s.dst, bytes(s.n, s.dst_type), true);
     }
-    if (!writes || ranges.size() < 2) return;
-    std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
-    uintptr_t read = 0, written = 0;  // where the ranges before end
-    for (const Range& r : ranges) {
-        if (r.from < written || (r.written && r.from < read)) refuse("a tensor that is written to shares memory with another one of the call");
-        (r.written ? written : read) = std::max(r.written ? written : read, r.to);
-    }
+    ranges.check_apart();
 }
 
 // clip(device, stream, grads, outs, max_norm): outs is grads for clipping in place, None for the norm alone.
@@ -366,8 +382,256 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Whether the rows of a matrix share memory with those of another.  Matrices side by side in one buffer do not.
+bool share(const Rows& a, int64_t asize, const Rows& b, int64_t bsize) {
+    if (a.n == 0 || a.dim == 0 || b.n == 0 || b.dim == 0) return false;
+    const auto end = [](const Rows& r, int64_t size) { return reinterpret_cast<uintptr_t>(r.data) + (uintptr_t)(((r.n - 1) * r.stride + r.dim) * size); };
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.data), pb = reinterpret_cast<uintptr_t>(b.data);
+    if (pa >= end(b, bsize) || pb >= end(a, asize)) return false;
+    const uintptr_t step = (uintptr_t)(a.stride * asize), wa = (uintptr_t)(a.dim * asize), wb = (uintptr_t)(b.dim * bsize);
+    if (a.n < 2 || b.n < 2 || b.stride * bsize != a.stride * asize || wa > step || wb > step) return true;
+    const uintptr_t off = pb >= pa ? (pb - pa) % step : step - 1 - (pa - pb - 1) % step;  // of b's rows in a's
+    return off < wa || off + wb > step;
+}
+
+// Refuses an output that shares memory with an input, unless it takes its place.
+void check_place(const Rows& out, int64_t osize, const Rows& in, int64_t isize, const char* what, const char* which) {
+    const bool place = out.data == in.data && osize == isize && (out.stride == in.stride || out.n == 1);
+    if (!place && share(out, osize, in, isize)) refuse(std::string(what) + " shares memory with " + which + " without taking its place");
+}
+
+Rows vector_rows(const void* p, int64_t n) { return Rows{const_cast<void*>(p), p ? 1 : 0, n, n, 0}; }
+
+// A residual or a gradient that goes with x.
+Rows like(const at::Tensor& t, const at::Tensor& x, const char* what) {
+    if (t.scalar_type() != x.scalar_type() || t.sizes() != x.sizes() || t.device() != x.device()) refuse(std::string(what) + " must have x's type, shape and device");
+    return rows_of(t, what);
+}
+
+PyObject* wrap_or_none(const at::Tensor& t) {
+    if (!t.defined()) return none();
+    return THPVariable_Wrap(t);
+}
+
+// rms_norm(device, stream, x, weight, residual, eps, out, sum_out, group): group is None for an output of x's type, else the
+// columns of a scale of 8 bits, 0 for the row.
+PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Call c(args, n, 7);
+    const at::Tensor& x = c.tensor(0, "x");
+    const Rows r = rows_of(x, "x");
+    const at::Device device = x.device();
+    const bool eight = c.given(6);
+    const int64_t group = eight ? Call::number(c.args[6]) : 0;
+    const at::ScalarType param = c.given(1) ? c.tensor(1, "weight").scalar_type() : x.scalar_type();
+    const void* const w = c.given(1) ? vector_of(c.tensor(1, "weight"), "weight", param, r.dim, device) : nullptr;
+    const Rows res = c.given(2) ? like(c.tensor(2, "residual"), x, "residual") : Rows{nullptr, 0, 0, 0, 0};
+    if (c.given(5) && !c.given(2)) refuse("sum_out needs a residual");
+    if (!c.here(x)) return none();
+    const int64_t size = (int64_t)x.element_size();
+    at::Tensor y, scale, sum;
+    if (c.given(4)) {
+        y = c.tensor(4, "out");
+        check_writable(y, "out");
+        if (y.sizes() != x.sizes() || y.scalar_type() != (eight ? at::kFloat8_e4m3fn : x.scalar_type()) || y.device() != device)
+            refuse(std::string("out must have x's shape and device and the type ") + c10::toString(eight ? at::kFloat8_e4m3fn : x.scalar_type()));
+    } else {
+        y = fresh(x.sizes(), eight ? at::kFloat8_e4m3fn : x.scalar_type(), device);
+    }
+    const Rows o = rows_of(y, "out", eight);
+    if (c.given(2)) {
+        sum = c.given(5) ? c.tensor(5, "sum_out") : fresh(x.sizes(), x.scalar_type(), device);
+        if (c.given(5)) check_writable(sum, "sum_out");
+    }
+    const Rows h = c.given(2) ? like(sum, x, "sum_out") : Rows{nullptr, 0, 0, 0, 0};
+    if (c.given(4)) {
+        check_place(o, eight ? 1 : size, r, size, "out", "x");
+        check_place(o, eight ? 1 : size, res, size, "out", "residual");
+        if (share(o, eight ? 1 : size, vector_rows(w, r.dim), w ? (int64_t)c10::elementSize(param) : 1)) refuse("out shares memory with weight");
+    }
+    if (c.given(5)) {
+        check_place(h, size, r, size, "sum_out", "x");
+        check_place(h, size, res, size, "sum_out", "residual");
+        if (share(h, size, vector_rows(w, r.dim), w ? (int64_t)c10::elementSize(param) : 1)) refuse("sum_out shares memory with weight");
+        if (share(o, eight ? 1 : size, h, size)) refuse("out shares memory with sum_out");
+    }
+    const auto lead = x.sizes().slice(0, x.dim() - 1);
+    if (eight) scale = group ? fresh(shape_of(lead, group > 0 ? (r.dim + group - 1) / group : 0), at::kFloat, device) : fresh(lead, at::kFloat, device);
+    const at::Tensor rstd = fresh(lead, at::kFloat, device);
+    check(scd_rms_norm(r.data, r.type, r.stride, res.data, res.stride, r.n, r.dim, w, element(param), Call::real(c.args[3]), o.data, eight ? SCD_E4M3 : r.type, o.stride,
+                       eight ? static_cast<float*>(scale.data_ptr()) : nullptr, group, h.data, h.stride, static_cast<float*>(rstd.data_ptr()), c.stream));
+    if (c.given(4)) written(y);
+    if (c.given(5)) written(sum);
+    PyObject* const kept = sum.defined() ? THPVariable_Wrap(sum) : Py_NewRef(c.args[0]);
+    if (eight) return Py_BuildValue("(NNNN)", THPVariable_Wrap(y), THPVariable_Wrap(scale), THPVariable_Wrap(rstd), kept);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(y), THPVariable_Wrap(rstd), kept);
+    END_HANDLE_TH_ERRORS
+}
+
+// rms_norm_grad(device, stream, grad, x, rstd, weight, residual_grad, params, out)
+PyObject* rms_norm_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Call c(args, n, 7);
+    const at::Tensor &grad = c.tensor(0, "grad"), &x = c.tensor(1, "x");
+    const Rows r = rows_of(x, "x"), g = like(grad, x, "grad");
+    const at::Device device = x.device();
+    const void* const s = vector_of(c.tensor(2, "rstd"), "rstd", at::kFloat, r.n, device);
+    const at::ScalarType param = c.given(3) ? c.tensor(3, "weight").scalar_type() : x.scalar_type();
+    const void* const w = c.given(3) ? vector_of(c.tensor(3, "weight"), "weight", param, r.dim, device) : nullptr;
+    const Rows res = c.given(4) ? like(c.tensor(4, "residual_grad"), x, "residual_grad") : Rows{nullptr, 0, 0, 0, 0};
+    const int params = PyObject_IsTrue(c.args[5]);
+    if (params < 0) throw python_error();
+    if (!c.here(x)) return none();
+    const Output o = output(c, 6, x.sizes(), x.scalar_type(), device);
+    if (o.given) {
+        const int64_t size = (int64_t)x.element_size();
+        check_place(o.rows, size, g, size, "out", "grad");
+        check_place(o.rows, size, r, size, "out", "x");
+        check_place(o.rows, size, res, size, "out", "residual_grad");
+        if (share(o.rows, size, vector_rows(s, r.n), 4)) refuse("out shares memory with rstd");
+        if (share(o.rows, size, vector_rows(w, r.dim), w ? (int64_t)c10::elementSize(param) : 1)) refuse("out shares memory with weight");
+    }
+    at::Tensor dw;
+    int64_t need = 0;
+    if (params) {
+        check(scd_rms_norm_grad_workspace(r.n, r.dim, &need));
+        dw = fresh({r.dim}, param, device);
+    }
+    const Scratch work(need);
+    check(scd_rms_norm_grad(g.data, g.stride, r.data, r.stride, r.type, static_cast<const float*>(s), r.n, r.dim, w, element(param), res.data, res.stride,
+                            o.rows.data, o.rows.stride, params ? dw.data_ptr() : nullptr, work.data.get(), need, c.stream));
+    o.done();
+    return Py_BuildValue("(NN)", THPVariable_Wrap(o.t), wrap_or_none(dw));
+    END_HANDLE_TH_ERRORS
+}
+
+// A sequence argument, as a list or tuple.
+THPObjectPtr sequence(PyObject* o, const char* what) {
+    THPObjectPtr s(PySequence_Fast(o, (std::string(what) + " must be a sequence").c_str()));
+    if (!s) throw python_error();
+    return s;
+}
+
+const at::Tensor& item(PyObject* list, Py_ssize_t i, const char* what) {
+    PyObject* const p = PySequence_Fast_GET_ITEM(list, i);
+    if (!THPVariable_Check(p)) refuse(std::string(what) + " must be tensors");
+    return THPVariable_Unpack(p);
+}
+
+// A device scalar of the given type.
+const at::Tensor& scalar(const Call& c, int k, const char* what, at::ScalarType type, const at::Device& device) {
+    const at::Tensor& t = c.tensor(k, what);
+    vector_of(t, what, type, 1, device);
+    return t;
+}
+
+// adamw(device, stream, params, grads, state, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm, copies, seed): step and
+// lr are numbers or device scalars, weight_decay a number or a sequence of them.
+PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Call c(args, n, 13);
+    THPObjectPtr params = sequence(c.args[0], "params"), grads = sequence(c.args[1], "grads"), states = sequence(c.args[2], "state");
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(params.get());
+    if (count == 0) refuse("no parameters");
+    if (PySequence_Fast_GET_SIZE(grads.get()) != count || PySequence_Fast_GET_SIZE(states.get()) != count)
+        refuse("params, grads and state must have as many entries");
+    THPObjectPtr copies, decays;
+    if (c.given(11)) {
+        copies = sequence(c.args[11], "copies");
+        if (PySequence_Fast_GET_SIZE(copies.get()) != count) refuse("copies must have as many entries as params");
+    }
+    float decay = 0.0f;
+    if (PySequence_Check(c.args[8])) {
+        decays = sequence(c.args[8], "weight_decay");
+        if (PySequence_Fast_GET_SIZE(decays.get()) != count) refuse("weight_decay must have as many entries as params");
+    } else {
+        decay = Call::real(c.args[8]);
+    }
+    const at::Device device = item(params.get(), 0, "params").device();
+    if (!device.is_cuda()) refuse("params must be CUDA tensors");
+    std::vector<scd_adamw_span_t> spans((size_t)count);
+    std::vector<const at::Tensor*> writes;
+    writes.reserve((size_t)count * 6);
+    Ranges ranges;
+    ranges.all.reserve((size_t)count * 7 + 3);
+    // A tensor of the call that belongs to the i-th parameter.
+    const auto take = [&](const at::Tensor& t, const char* what, Py_ssize_t i, at::IntArrayRef sizes, bool write) {
+        if (t.device() != device || t.sizes() != sizes || !t.is_contiguous())
+            refuse(std::string(what) + " " + std::to_string(i) + " must be contiguous, with its parameter's shape, on the first parameter's GPU");
+        if (write) {
+            if (t.requires_grad()) check_writable(t, std::string(what) + " " + std::to_string(i));
+            writes.push_back(&t);
+        }
+        ranges.add(t, write);
+        return t.data_ptr();
+    };
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor &p = item(params.get(), i, "params"), &g = item(grads.get(), i, "grads");
+        scd_adamw_span_t& s = spans[(size_t)i];
+        s = scd_adamw_span_t{};
+        const auto sizes = p.sizes();
+        s.n = p.numel();
+        s.param_type = element(p.scalar_type());
+        s.grad_type = element(g.scalar_type());
+        if (s.param_type < 0 || s.grad_type < 0) refuse("params and grads must be float32, bfloat16 or float16");
+        s.param = take(p, "parameter", i, sizes, true);
+        s.grad = take(g, "gradient", i, sizes, false);
+        PyObject* const state = PySequence_Fast_GET_ITEM(states.get(), i);
+        const Py_ssize_t parts = PyTuple_Check(state) || PyList_Check(state) ? PySequence_Fast_GET_SIZE(state) : 0;
+        if (parts != 2 && parts != 4) refuse("an entry of state has two tensors (32 bits) or four (8 bits)");
+        const at::ScalarType held = parts == 2 ? at::kFloat : at::kFloat8_e4m3fn;
+        const at::Tensor &m = item(state, 0, "states"), &v = item(state, 1, "states");
+        if (m.scalar_type() != held || v.scalar_type() != held) refuse(std::string("state ") + std::to_string(i) + " must be of the type " + c10::toString(held));
+        s.m = take(m, "state", i, sizes, true);
+        s.v = take(v, "state", i, sizes, true);
+        s.state_type = parts == 2 ? SCD_F32 : SCD_E4M3;
+        if (parts == 4) {
+            const int64_t blocks[1] = {(s.n + 255) / 256};
+            const at::Tensor &ms = item(state, 2, "states"), &vs = item(state, 3, "states");
+            if (ms.scalar_type() != at::kFloat || vs.scalar_type() != at::kFloat || ms.sizes() != at::IntArrayRef(blocks) || vs.sizes() != at::IntArrayRef(blocks))
+                refuse("scales of state " + std::to_string(i) + " must be float32 with one element for each 256 of the parameter");
+            s.m_scale = static_cast<float*>(take(ms, "scales of state", i, blocks, true));
+            s.v_scale = static_cast<float*>(take(vs, "scales of state", i, blocks, true));
+        }
+        if (copies && PySequence_Fast_GET_ITEM(copies.get(), i) != Py_None) {
+            const at::Tensor& q = item(copies.get(), i, "copies");
+            s.copy_type = element(q.scalar_type());
+            if (s.param_type != SCD_F32 || (s.copy_type != SCD_BF16 && s.copy_type != SCD_F16)) refuse("copies must be bfloat16 or float16, of float32 parameters");
+            s.copy = take(q, "copy", i, sizes, true);
+        }
+        s.weight_decay = decays ? Call::real(PySequence_Fast_GET_ITEM(decays.get(), i)) : decay;
+    }
+    scd_adamw_t o{};
+    const auto read = [&](const at::Tensor& t) {
+        ranges.add(t, false);
+        return t.data_ptr();
+    };
+    if (THPVariable_Check(c.args[3]))
+        o.step_dev = static_cast<const int64_t*>(read(scalar(c, 3, "step", at::kLong, device)));
+    else
+        o.step = Call::number(c.args[3]);
+    if (THPVariable_Check(c.args[4]))
+        o.lr_dev = static_cast<const float*>(read(scalar(c, 4, "lr", at::kFloat, device)));
+    else
+        o.lr = Call::real64(c.args[4]);
+    if (c.given(9)) o.norm_dev = static_cast<const float*>(read(scalar(c, 9, "norm", at::kFloat, device)));
+    o.beta1 = Call::real64(c.args[5]);
+    o.beta2 = Call::real64(c.args[6]);
+    o.eps = Call::real64(c.args[7]);
+    o.max_norm = Call::real(c.args[10]);
+    const int64_t seed = Call::number(c.args[12]);
+    if (seed < 0 || seed > 0xFFFFFFFFLL) refuse("seed must be in [0, 2^32)");
+    o.seed = (uint32_t)seed;
+    ranges.check_apart();
+    if (device.index() != c.device) return none();
+    check(scd_adamw(spans.data(), count, &o, c.stream));
+    for (const at::Tensor* t : writes) written(*t);
+    return Py_NewRef(Py_True);
+    END_HANDLE_TH_ERRORS
+}
+
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(embed), ENTRY(embed_grad), ENTRY(layer_norm), ENTRY(layer_norm_grad), ENTRY(clip), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ENTRY(embed), ENTRY(embed_grad), ENTRY(layer_norm), ENTRY(layer_norm_grad), ENTRY(clip), ENTRY(rms_norm), ENTRY(rms_norm_grad), ENTRY(adamw), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_features", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -15,55 +15,11 @@
 
 #include "scd_device.h"
 #include "scd_feat.h"
+#include "scd_rows.h"
 
 namespace scd {
 namespace feat {
 namespace {
-
-// The columns of a lane's NV vectors: vector j of lane l is the (l + j LPR)-th of the row.
-template <int VEC, int NV, int LPR>
-struct Columns {
-    int32_t at[NV];
-    int32_t skip[NV];  // leading columns that another lane counts; VEC where the row has no such vector
-    __device__ __forceinline__ Columns(int32_t lane, int32_t dim) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int32_t k = lane + j * LPR;
-            at[j] = vec_column<VEC>(k, dim, skip[j]);
-            skip[j] = min(skip[j], VEC);
-        }
-    }
-};
-
-// The sums of K values over each group of LPR lanes.  Groups wider than a wave go through LDS; `turn` alternates
-// from call to call, so that one barrier a call is enough.
-template <int LPR, int THREADS, int K>
-__device__ __forceinline__ void group_sums(float (&s)[K], float* lds, int turn) {
-    if constexpr (LPR <= 64) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) s[k] = group_sum<LPR>(s[k]);
-    } else {
-        constexpr int kWaves = LPR / 64;
-        float* const mine = lds + turn * (THREADS / 64) * K + (threadIdx.x / LPR) * kWaves * K;
-#pragma unroll
-        for (int k = 0; k < K; ++k) s[k] = group_sum<64>(s[k]);
-        if (threadIdx.x % 64 == 0)
-#pragma unroll
-            for (int k = 0; k < K; ++k) mine[threadIdx.x % LPR / 64 * K + k] = s[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            s[k] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) s[k] += mine[w * K + k];
-        }
-    }
-}
-
-template <int LPR, int THREADS>
-constexpr int lds_words(int k) {
-    return LPR <= 64 ? 1 : 2 * (THREADS / 64) * k;
-}
 
 template <typename T, typename P>
 struct NormArgs {
@@ -162,7 +118,6 @@ __global__ void __launch_bounds__(THREADS) k_norm(NormArgs<T, P> a) {
 // Rows too wide for the registers: a workgroup reads its row three times (from the caches after the first), element by
 // element, which bounds it: 4,096 x 32,768 forward 458 us in bf16 (1.2 TB/s) and 404 in fp32 (2.7 TB/s); backward, where dw
 // and db go through the workspace with every row, 800 (1.0 TB/s) and 990 (1.6 TB/s).
-constexpr int kWideThreads = 1024;
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(kWideThreads) k_norm_wide(NormArgs<T, P> a) {
@@ -402,64 +357,12 @@ __global__ void __launch_bounds__(64 * kSlices) k_norm_params(const float* __res
 
 // ---------------------------------------------------------------------------------------- host
 
-// Calls f(Int<VEC>, Int<NV>, Int<LPR>) with the smallest group that holds a row of `dim` elements of T, or returns
-// false where none does.  A wave holds four vectors a lane, but in the backward pass, which keeps six values per element,
-// of 16-bit elements three; and the widest rows take 512 threads there, which may have 256 registers each, and 1,024 in
-// the forward pass.
-template <typename T, bool GRAD, typename F>
-bool with_group(int64_t dim, F&& f) {
-    constexpr int V = 16 / sizeof(T);
-    const int64_t vecs = ceil_div(dim, V);
-    if (dim < V)
-        f(Int<1>{}, Int<1>{}, Int<8>{});
-    else if (vecs <= 4)
-        f(Int<V>{}, Int<1>{}, Int<4>{});
-    else if (vecs <= 8)
-        f(Int<V>{}, Int<1>{}, Int<8>{});
-    else if (vecs <= 16)
-        f(Int<V>{}, Int<1>{}, Int<16>{});
-    else if (vecs <= 32)
-        f(Int<V>{}, Int<1>{}, Int<32>{});
-    else if (vecs <= 64)
-        f(Int<V>{}, Int<1>{}, Int<64>{});
-    else if (vecs <= 128)
-        f(Int<V>{}, Int<2>{}, Int<64>{});
-    else if (vecs <= 192)
-        f(Int<V>{}, Int<3>{}, Int<64>{});
-    else if (vecs <= 256)
-        f(Int<V>{}, Int<GRAD && V == 8 ? 1 : 4>{}, Int<GRAD && V == 8 ? 256 : 64>{});
-    else if (vecs <= 512)
-        f(Int<V>{}, Int<2>{}, Int<256>{});
-    else if (vecs <= 1024)
-        f(Int<V>{}, Int<2>{}, Int<512>{});
-    else if (vecs <= 2048)
-        f(Int<V>{}, Int<GRAD ? 4 : 2>{}, Int<GRAD ? 512 : 1024>{});
-    else if constexpr (V == 4) {
-        if (vecs > 4096) return false;
-        f(Int<V>{}, Int<GRAD ? 8 : 4>{}, Int<GRAD ? 512 : 1024>{});
-    } else {
-        return false;
-    }
-    return true;
-}
-
 constexpr int kNormThreads = 256;   // a workgroup, where a row's group is not wider
 constexpr int kBlocks = 2048;       // workgroups at most: eight to each CU
 // The backward pass's, whose sums of dw and db go through memory: two to a CU, or one where a row takes 512 threads, whose
 // registers fill the CU (8,192 x 8,192 in bf16: 89 us with two, 83 with one).
 constexpr int kGradBlocks = 512;
 constexpr int kGradBlocksWide = 256;
-
-template <typename F>
-void with_types(int32_t type, int32_t param, F&& f) {
-    with_type(type, [&](auto t) {
-        using T = decltype(t);
-        if constexpr (sizeof(T) == 4)
-            f(t, t);
-        else
-            param == SCD_F32 ? f(t, float{}) : f(t, t);
-    });
-}
 
 int check_norm(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {
     if (!type_bytes(type) || (param_type != type && param_type != SCD_F32))

@@ -1,0 +1,630 @@
+// scd_rms.hip -- root-mean-square norm over the columns of a matrix, with the residual's addition and an output in 8 bits,
+// and its gradient (gfx950).
+//
+// Forward: h = x + residual, rounded to the elements' type; r = 1/sqrt(mean h^2 + eps), y = h r w.  The norm is of the
+// rounded h, which the caller keeps: the gradient reads it, and is that of the values that were used.
+// In 8 bits: q = y / s rounded once from 32 bits, s = max |y| / 448 over the row or over groups of its columns.
+// Backward, n = h r, g = dy w:  dh = r (g - n mean(g n)) (+ the residual's gradient), dw = sum_rows dy n.
+//
+// All are bound by memory: every matrix is read or written once.  A row stays in the registers of a group of lanes
+// between its statistics and its result; groups walk the rows with a fixed stride and load the next row before they work
+// on this one.  The backward pass keeps its share of dw in registers on the way, each workgroup writes its sums to the
+// workspace in 32 bits, and a second kernel adds them in a fixed order.
+#include <algorithm>
+
+#include "scd_device.h"
+#include "scd_e4m3.h"
+#include "scd_feat.h"
+#include "scd_rows.h"
+
+namespace scd {
+namespace feat {
+namespace {
+
+template <typename T, typename P>
+struct RmsArgs {
+    const T* x;
+    int64_t xstride;
+    const T* res;  // or null
+    int64_t rstride;
+    int32_t rows;
+    int32_t dim;
+    const P* weight;
+    float eps;
+    int32_t group;   // columns of a scale, 0: the row
+    int32_t scales;  // of a row
+    void* y;         // of T, or of 8 bits
+    int64_t ystride;
+    float* scale;
+    T* sum;  // x + res, not null with res
+    int64_t sstride;
+    float* rstd;
+};
+
+// The values of a vector in 8 bits, from the `skip`-th on.
+template <int VEC>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&v)[VEC], int32_t skip) {
+    if constexpr (VEC == 1) {
+        *p = (uint8_t)e4m3_pack4(v[0], 0.0f, 0.0f, 0.0f);
+    } else {
+        uint32_t w[VEC / 4];
+#pragma unroll
+        for (int i = 0; i < VEC / 4; ++i) w[i] = e4m3_pack4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        if (skip == 0) {
+            __builtin_memcpy(p, w, sizeof w);
+        } else {  // the columns before may have another scale
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (i >= skip) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+        }
+    }
+}
+
+// max |x| over each group of LPR lanes; groups wider than a wave go through LDS as group_sums does.
+template <int LPR, int THREADS>
+__device__ __forceinline__ float row_max(float x, float* lds, int turn) {
+    if constexpr (LPR <= 64) {
+        return group_max<LPR>(x, LPR);
+    } else {
+        constexpr int kWaves = LPR / 64;
+        float* const mine = lds + turn * (THREADS / 64) + (threadIdx.x / LPR) * kWaves;
+        x = group_max<64>(x, 64);
+        if (threadIdx.x % 64 == 0) mine[threadIdx.x % LPR / 64] = x;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x = fmaxf(x, mine[w]);
+        return x;
+    }
+}
+
+// Q: the output in 8 bits.  ONCE: large outputs go past the caches.
+template <int VEC, int NV, int LPR, int THREADS, bool Q, bool ONCE, typename T, typename P>
+__global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
+    __shared__ float lds[lds_words<LPR, THREADS>(1)];
+    constexpr int kGroups = THREADS / LPR;
+    const int32_t lane = threadIdx.x % LPR;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const Columns<VEC, NV, LPR> col(lane, a.dim);
+    const float inv = 1.0f / (float)a.dim;
+    Raw<VEC, T> next[NV], more[NV];
+    Raw<VEC, P> w[NV];
+    const auto fetch = [&](int64_t row) {
+        row = min(row, (int64_t)a.rows - 1);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) next[j] = load_raw<VEC>(a.x + row * a.xstride + col.at[j]);
+        if (a.res)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) more[j] = load_raw<VEC>(a.res + row * a.rstride + col.at[j]);
+    };
+    fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
+    if (a.weight)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) w[j] = load_raw<VEC>(a.weight + col.at[j]);
+    else
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[j].t[i] = (P)1.0f;
+    int turn = 0;
+    // Every group of a workgroup takes as many turns, those past the last row on that row and without a result.
+    for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < a.rows; r0 += step) {
+        const int64_t r = r0 + threadIdx.x / LPR;
+        const bool here = r < a.rows;
+        float h[NV][VEC];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) widen(next[j], h[j]);
+        if (a.res) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                Raw<VEC, T> sum;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    sum.t[i] = (T)(h[j][i] + (float)more[j].t[i]);
+                    h[j][i] = (float)sum.t[i];
+                }
+                if (here && col.skip[j] < VEC) put_vec<ONCE>(a.sum + r * a.sstride + col.at[j], h[j]);
+            }
+        }
+        if (r0 + step < a.rows) fetch(r + step);
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s[0] += i >= col.skip[j] ? h[j][i] * h[j][i] : 0.0f;
+        group_sums<LPR, THREADS, 1>(s, lds, turn);
+        turn ^= 1;
+        const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
+        float most = 0.0f, part[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float wj[VEC];
+            widen(w[j], wj);
+            part[j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                h[j][i] = h[j][i] * rstd * wj[i];
+                if (Q) part[j] = fmaxf(part[j], i >= col.skip[j] ? fabsf(h[j][i]) : 0.0f);
+            }
+            if (Q) most = fmaxf(most, part[j]);
+        }
+        if constexpr (Q) {
+            float scale = 0.0f, to = 0.0f;
+            if (a.group == 0) {
+                scale = e4m3_scale(row_max<LPR, THREADS>(most, lds, turn));
+                turn ^= 1;
+                to = 1.0f / scale;
+                if (here && lane == 0) a.scale[r] = scale;
+            }
+            const int lanes = min(a.group / VEC, LPR);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (a.group) {
+                    scale = e4m3_scale(group_max<(LPR < 32 ? LPR : 32)>(part[j], lanes));
+                    to = 1.0f / scale;
+                    const int32_t c = (lane + j * LPR) * VEC;
+                    if (here && c < a.dim && c % a.group == 0) a.scale[r * a.scales + c / a.group] = scale;
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) h[j][i] *= to;
+                if (here && col.skip[j] < VEC) store_e4m3<VEC>((uint8_t*)a.y + r * a.ystride + col.at[j], h[j], col.skip[j]);
+            }
+        } else if (here) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (col.skip[j] < VEC) put_vec<ONCE>((T*)a.y + r * a.ystride + col.at[j], h[j]);
+        }
+        if (here && lane == 0 && a.rstd) a.rstd[r] = rstd;
+    }
+}
+
+// n of a vector's elements, the rest zeros.
+template <int V, typename T>
+__device__ __forceinline__ void load_some(const T* p, int32_t n, float (&o)[V]) {
+    if (n >= V) {
+        load_vec(p, o);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = i < n ? (float)p[i] : 0.0f;
+    }
+}
+
+template <int V, typename T>
+__device__ __forceinline__ void store_some(T* p, int32_t n, const float (&v)[V]) {
+    if (n >= V) {
+        store_vec(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = (T)v[i];
+    }
+}
+
+// Rows too wide for the registers: a workgroup reads its row again from the caches, twice, or three times where 8 bits with
+// one scale for the row need the largest value first.  Each thread reads again what it wrote itself.
+template <bool Q, typename T, typename P>
+__global__ void __launch_bounds__(kWideThreads) k_rms_wide(RmsArgs<T, P> a) {
+    constexpr int V = 16 / sizeof(T), kStep = kWideThreads * V;
+    __shared__ float lds[lds_words<kWideThreads, kWideThreads>(1)];
+    const float inv = 1.0f / (float)a.dim;
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T* const x = a.x + r * a.xstride;
+        const T* const res = a.res ? a.res + r * a.rstride : nullptr;
+        T* const sum = a.sum ? a.sum + r * a.sstride : nullptr;
+        const T* const kept = res ? sum : x;
+        float s[1] = {0.0f};
+        for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
+            const int32_t n = min(V, a.dim - c);
+            float h[V];
+            load_some(x + c, n, h);
+            if (res) {
+                float more[V];
+                load_some(res + c, n, more);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[i] = (float)(T)(h[i] + more[i]);
+                store_some(sum + c, n, h);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += h[i] * h[i];
+        }
+        group_sums<kWideThreads, kWideThreads, 1>(s, lds, turn);
+        turn ^= 1;
+        const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
+        const auto result = [&](int32_t c, int32_t n, float(&y)[V]) {
+            float w[V];
+            load_some(kept + c, n, y);
+            if (a.weight) load_some(a.weight + c, n, w);
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = y[i] * rstd * (a.weight ? w[i] : 1.0f);
+        };
+        const auto largest = [&](const float(&y)[V]) {
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) most = fmaxf(most, fabsf(y[i]));
+            return most;
+        };
+        if constexpr (Q) {
+            float scale = 0.0f;
+            if (a.group == 0) {
+                float most = 0.0f;
+                for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
+                    float y[V];
+                    result(c, min(V, a.dim - c), y);
+                    most = fmaxf(most, largest(y));
+                }
+                scale = e4m3_scale(row_max<kWideThreads, kWideThreads>(most, lds, turn));
+                turn ^= 1;
+                if (threadIdx.x == 0) a.scale[r] = scale;
+            }
+            uint8_t* const q = (uint8_t*)a.y + r * a.ystride;
+            for (int32_t c0 = 0; c0 < a.dim; c0 += kStep) {  // all lanes of a wave go on to its groups' last one
+                const int32_t c = c0 + threadIdx.x * V, n = min(V, a.dim - c);
+                float y[V] = {};
+                if (n > 0) result(c, n, y);
+                if (a.group) {
+                    scale = e4m3_scale(group_max<32>(largest(y), a.group / V));
+                    if (n > 0 && c % a.group == 0) a.scale[r * a.scales + c / a.group] = scale;
+                }
+                const float to = 1.0f / scale;
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] *= to;
+                if (n == V) {
+                    store_e4m3<V>(q + c, y, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (i < n) q[c + i] = (uint8_t)e4m3_pack4(y[i], 0.0f, 0.0f, 0.0f);
+                }
+            }
+        } else {
+            T* const y = (T*)a.y + r * a.ystride;
+            for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
+                const int32_t n = min(V, a.dim - c);
+                float o[V];
+                result(c, n, o);
+                store_some(y + c, n, o);
+            }
+        }
+        if (threadIdx.x == 0 && a.rstd) a.rstd[r] = rstd;
+    }
+}
+
+// ---------------------------------------------------------------------------------------- backward
+
+template <typename T, typename P>
+struct RmsGradArgs {
+    const T* dy;
+    int64_t gstride;
+    const T* h;
+    int64_t hstride;
+    const T* res;  // the residual's gradient, or null
+    int64_t rstride;
+    const float* rstd;
+    int32_t rows;
+    int32_t dim;
+    const P* weight;
+    T* dh;
+    int64_t dstride;
+    float* sums;  // [workgroups][dim] of dw, or null
+    P* dw;        // not null with one workgroup: its sums are the result
+};
+
+template <int VEC, int NV, int LPR, int THREADS, bool ONCE, typename T, typename P>
+__global__ void __launch_bounds__(THREADS) k_rms_grad(RmsGradArgs<T, P> a) {
+    constexpr int kGroups = THREADS / LPR;
+    constexpr int kElems = LPR * NV * VEC;
+    __shared__ float lds[lds_words<LPR, THREADS>(1)];
+    __shared__ float part[kGroups > 1 ? kGroups * kElems : 1];
+    // The weights stay in registers, but not where a thread's share of the row leaves none for them: then each row reads
+    // them from the caches.
+    constexpr bool kWeights = NV * VEC <= 16;
+    const int32_t lane = threadIdx.x % LPR;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const Columns<VEC, NV, LPR> col(lane, a.dim);
+    const float inv = 1.0f / (float)a.dim;
+    Raw<VEC, T> ndy[NV], nh[NV], nres[NV];
+    Raw<VEC, P> w[NV];
+    float nrstd, dw[NV][VEC] = {};
+    const auto fetch = [&](int64_t row) {
+        row = min(row, (int64_t)a.rows - 1);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) ndy[j] = fetch_raw<VEC, ONCE>(a.dy + row * a.gstride + col.at[j]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) nh[j] = fetch_raw<VEC, ONCE>(a.h + row * a.hstride + col.at[j]);
+        if (a.res)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) nres[j] = fetch_raw<VEC, ONCE>(a.res + row * a.rstride + col.at[j]);
+        nrstd = a.rstd[row];
+    };
+    fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
+    const auto weights = [&](int j) {
+        if (a.weight)
+            w[j] = load_raw<VEC>(a.weight + col.at[j]);
+        else
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[j].t[i] = (P)1.0f;
+    };
+    if (kWeights)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) weights(j);
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
+        const int64_t r = r0 + threadIdx.x / LPR;
+        const bool here = r < a.rows;
+        const float rstd = nrstd;
+        float g[NV][VEC], n[NV][VEC], res[NV][VEC], s[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            widen(ndy[j], g[j]);
+            widen(nh[j], n[j]);
+            if (a.res)
+                widen(nres[j], res[j]);
+            else
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) res[j][i] = 0.0f;
+        }
+        if (r0 + step < a.rows) fetch(r + step);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float wj[VEC];
+            if (!kWeights) weights(j);
+            widen(w[j], wj);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                n[j][i] *= rstd;
+                if (here) dw[j][i] += g[j][i] * n[j][i];
+                g[j][i] *= wj[i];
+                s[0] += i >= col.skip[j] ? g[j][i] * n[j][i] : 0.0f;
+            }
+        }
+        group_sums<LPR, THREADS, 1>(s, lds, turn);
+        const float c = s[0] * inv;
+        if (here) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) g[j][i] = rstd * (g[j][i] - n[j][i] * c) + res[j][i];
+                if (col.skip[j] < VEC) put_vec<ONCE>(a.dh + r * a.dstride + col.at[j], g[j]);
+            }
+        }
+    }
+    if (!a.sums && !a.dw) return;
+    float* const sums = a.sums + (int64_t)blockIdx.x * a.dim;
+    if constexpr (kGroups > 1) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) part[(threadIdx.x / LPR) * kElems + (lane + j * LPR) * VEC + i] = dw[j][i];
+        __syncthreads();
+        for (int e = threadIdx.x; e < kElems; e += THREADS) {
+            int32_t again;
+            const int32_t c = vec_column<VEC>(e / VEC, a.dim, again) + e % VEC;
+            if (e % VEC < again) continue;
+            float s = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) s += part[k * kElems + e];
+            if (a.dw)
+                a.dw[c] = (P)s;
+            else
+                sums[c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (col.skip[j] < VEC) {
+                if (a.dw)
+                    store_vec(a.dw + col.at[j], dw[j]);
+                else
+                    store_vec(sums + col.at[j], dw[j]);
+            }
+    }
+}
+
+// Wide rows: dw by columns, which the row kernel after it may overwrite the inputs of.  A thread takes a vector of columns
+// and every gridDim.y-th row.
+constexpr int kColumnThreads = 256;
+
+template <typename T, typename P>
+__global__ void __launch_bounds__(kColumnThreads) k_rms_columns(RmsGradArgs<T, P> a) {
+    constexpr int V = 16 / sizeof(T);
+    const int32_t c = (blockIdx.x * kColumnThreads + threadIdx.x) * V, n = min(V, a.dim - c);
+    if (n <= 0) return;
+    float dw[V] = {};
+#pragma unroll 4
+    for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
+        const float rstd = a.rstd[r];
+        float g[V], h[V];
+        load_some(a.dy + r * a.gstride + c, n, g);
+        load_some(a.h + r * a.hstride + c, n, h);
+#pragma unroll
+        for (int i = 0; i < V; ++i) dw[i] += g[i] * (h[i] * rstd);
+    }
+    if (a.dw)
+        store_some(a.dw + c, n, dw);
+    else
+        store_some(a.sums + (int64_t)blockIdx.y * a.dim + c, n, dw);
+}
+
+template <typename T, typename P>
+__global__ void __launch_bounds__(kWideThreads) k_rms_grad_wide(RmsGradArgs<T, P> a) {
+    constexpr int V = 16 / sizeof(T), kStep = kWideThreads * V;
+    __shared__ float lds[lds_words<kWideThreads, kWideThreads>(1)];
+    const float inv = 1.0f / (float)a.dim;
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+        const float rstd = a.rstd[r];
+        const auto load = [&](int32_t c, int32_t k, float(&g)[V], float(&n)[V]) {
+            load_some(a.dy + r * a.gstride + c, k, g);
+            load_some(a.h + r * a.hstride + c, k, n);
+            float w[V];
+            if (a.weight) load_some(a.weight + c, k, w);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                n[i] *= rstd;
+                g[i] *= a.weight ? w[i] : 1.0f;
+            }
+        };
+        float s[1] = {0.0f};
+        for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
+            float g[V], n[V];
+            load(c, min(V, a.dim - c), g, n);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += g[i] * n[i];
+        }
+        group_sums<kWideThreads, kWideThreads, 1>(s, lds, turn);
+        const float mean = s[0] * inv;
+        for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
+            const int32_t k = min(V, a.dim - c);
+            float g[V], n[V], res[V] = {};
+            load(c, k, g, n);
+            if (a.res) load_some(a.res + r * a.rstride + c, k, res);
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = rstd * (g[i] - n[i] * mean) + res[i];
+            store_some(a.dh + r * a.dstride + c, k, g);
+        }
+    }
+}
+
+// dw: the workgroups' sums, 64 columns a workgroup, in kSlices interleaved parts that are added in order.
+constexpr int kSlices = 16;
+
+template <typename P>
+__global__ void __launch_bounds__(64 * kSlices) k_rms_params(const float* __restrict__ sums, int32_t parts, int32_t dim, P* __restrict__ dw) {
+    __shared__ float lds[kSlices][64];
+    const int32_t c = blockIdx.x * 64 + threadIdx.x % 64, slice = threadIdx.x / 64;
+    float s = 0.0f;
+    if (c < dim)
+#pragma unroll 8
+        for (int32_t p = slice; p < parts; p += kSlices) s += sums[(int64_t)p * dim + c];
+    lds[slice][threadIdx.x % 64] = s;
+    __syncthreads();
+    if (slice == 0 && c < dim) {
+#pragma unroll
+        for (int k = 1; k < kSlices; ++k) s += lds[k][threadIdx.x];
+        dw[c] = (P)s;
+    }
+}
+
+// ---------------------------------------------------------------------------------------- host
+
+constexpr int kRmsThreads = 256;      // a workgroup, where a row's group is not wider
+constexpr int kRmsBlocks = 2048;      // workgroups at most: eight to each CU
+constexpr int kRmsGradBlocks = 512;   // the backward pass's, whose sums of dw go through memory
+constexpr int kRmsGradBlocksWide = 256;
+constexpr int64_t kRmsTurnsAlone = 4;  // rows for each group of a workgroup up to which one workgroup does it all
+constexpr int64_t kRmsOnceOut = int64_t(64) << 20;
+constexpr int64_t kRmsOnceBytes = int64_t(288) << 20;
+
+int check_rms(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {
+    if (!type_bytes(type) || (param_type != type && param_type != SCD_F32))
+        return fail(SCD_ERR_UNSUPPORTED, "rms norm takes float32, bfloat16 or float16 with a weight of that type or float32");
+    if (rows < 0 || rows > kMaxRows || dim < 1 || dim > kMaxDim)
+        return fail(SCD_ERR_INVALID, "bad sizes rows=%lld dim=%lld", (long long)rows, (long long)dim);
+    return SCD_OK;
+}
+
+int64_t rms_grad_workspace(int64_t rows, int64_t dim) { return rows <= 1 ? 0 : std::min<int64_t>(rows, kRmsGradBlocks) * dim * 4; }
+
+}  // namespace
+}  // namespace feat
+}  // namespace scd
+
+using namespace scd::feat;
+
+extern "C" int scd_rms_norm(const void* x, int32_t type, int64_t x_stride, const void* residual, int64_t residual_stride, int64_t rows,
+                            int64_t dim, const void* weight, int32_t param_type, float eps, void* y, int32_t y_type, int64_t y_stride,
+                            float* scale, int64_t group, void* sum, int64_t sum_stride, float* rstd, void* stream) {
+    if (int r = check_rms(type, param_type, rows, dim)) return r;
+    if (y_type != type && y_type != SCD_E4M3) return fail(SCD_ERR_UNSUPPORTED, "rms norm gives its input's type or 8 bits (e4m3)");
+    if (!(eps >= 0.0f)) return fail(SCD_ERR_INVALID, "eps must be >= 0");
+    const bool eight = y_type == SCD_E4M3;
+    if (eight ? group != 0 && group != 32 && group != 64 && group != 128 : group != 0)
+        return fail(SCD_ERR_INVALID, "group must be 0 or, with 8 bits, 32, 64 or 128");
+    if (x_stride < 0 || (residual && residual_stride < 0) || (rows > 1 && (y_stride < dim || (residual && sum_stride < dim))))
+        return fail(SCD_ERR_INVALID, "bad row stride");
+    if (rows == 0) return SCD_OK;
+    if (!x || !y || (residual && !sum) || (eight && !scale)) return fail(SCD_ERR_INVALID, "null device pointer");
+    if ((residual && sum == y) || (eight && (y == x || y == residual))) return fail(SCD_ERR_INVALID, "outputs overlap");
+    if (rows > 1 && ((y == x && y_stride != x_stride) || (y == residual && y_stride != residual_stride) ||
+                     (residual && ((sum == x && sum_stride != x_stride) || (sum == residual && sum_stride != residual_stride)))))
+        return fail(SCD_ERR_INVALID, "in place the strides must be the same");
+    hipStream_t s = (hipStream_t)stream;
+    with_types(type, param_type, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        const RmsArgs<T, P> a{(const T*)x, x_stride, (const T*)residual, residual_stride, (int32_t)rows, (int32_t)dim, (const P*)weight, eps,
+                              (int32_t)group, (int32_t)(group ? ceil_div(dim, group) : 1), y, y_stride, scale, residual ? (T*)sum : nullptr, sum_stride, rstd};
+        const bool once = rows * dim * (int64_t)sizeof(T) >= kRmsOnceOut;
+        const bool fits = with_group<T, false>(dim, [&](auto vec, auto nv, auto lpr) {
+            constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
+            constexpr int THREADS = LPR > kRmsThreads ? LPR : kRmsThreads;
+            const uint32_t blocks = (uint32_t)std::min<int64_t>(kRmsBlocks, ceil_div(rows, THREADS / LPR));
+            if (eight)
+                once ? k_rms<VEC, NV, LPR, THREADS, true, true><<<blocks, THREADS, 0, s>>>(a) : k_rms<VEC, NV, LPR, THREADS, true, false><<<blocks, THREADS, 0, s>>>(a);
+            else
+                once ? k_rms<VEC, NV, LPR, THREADS, false, true><<<blocks, THREADS, 0, s>>>(a) : k_rms<VEC, NV, LPR, THREADS, false, false><<<blocks, THREADS, 0, s>>>(a);
+        });
+        const uint32_t blocks = (uint32_t)std::min<int64_t>(kRmsBlocks, rows);
+        if (!fits) eight ? k_rms_wide<true><<<blocks, kWideThreads, 0, s>>>(a) : k_rms_wide<false><<<blocks, kWideThreads, 0, s>>>(a);
+    });
+    return launched("scd_rms_norm");
+}
+
+extern "C" int scd_rms_norm_grad_workspace(int64_t rows, int64_t dim, int64_t* bytes) {
+    if (!bytes) return fail(SCD_ERR_INVALID, "bytes is null");
+    *bytes = 0;
+    if (int r = check_rms(SCD_F32, SCD_F32, rows, dim)) return r;
+    *bytes = rms_grad_workspace(rows, dim);
+    return SCD_OK;
+}
+
+extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const void* h, int64_t h_stride, int32_t type, const float* rstd,
+                                 int64_t rows, int64_t dim, const void* weight, int32_t param_type, const void* residual_grad,
+                                 int64_t residual_stride, void* dh, int64_t dh_stride, void* dweight, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+    if (int r = check_rms(type, param_type, rows, dim)) return r;
+    if (grad_stride < 0 || h_stride < 0 || (residual_grad && residual_stride < 0) || (dh_stride < dim && rows > 1))
+        return fail(SCD_ERR_INVALID, "bad row stride");
+    if (rows > 1 && ((dh == grad && dh_stride != grad_stride) || (dh == h && dh_stride != h_stride) ||
+                     (residual_grad && dh == residual_grad && dh_stride != residual_stride)))
+        return fail(SCD_ERR_INVALID, "in place the strides must be the same");
+    if (rows == 0 && !dweight) return SCD_OK;
+    if (rows > 0 && (!grad || !h || !rstd || !dh)) return fail(SCD_ERR_INVALID, "null device pointer");
+    const int64_t need = dweight ? rms_grad_workspace(rows, dim) : 0;
+    if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need))
+        return fail(SCD_ERR_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)need);
+    hipStream_t s = (hipStream_t)stream;
+    with_types(type, param_type, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        RmsGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)h, h_stride, (const T*)residual_grad, residual_stride, rstd, (int32_t)rows,
+                            (int32_t)dim, (const P*)weight, (T*)dh, dh_stride, nullptr, nullptr};
+        int64_t blocks = 0;  // whose sums go through the workspace
+        const bool fits = rows > 0 && with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
+            constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
+            constexpr int THREADS = LPR > kRmsThreads ? LPR : kRmsThreads;
+            constexpr int64_t groups = THREADS / LPR;
+            const bool alone = rows <= (LPR >= 512 ? 1 : kRmsTurnsAlone) * groups;
+            blocks = alone && dweight ? 1 : std::min<int64_t>(LPR >= 512 ? kRmsGradBlocksWide : kRmsGradBlocks, ceil_div(rows, groups));
+            a.dw = alone ? (P*)dweight : nullptr;
+            a.sums = alone || !dweight ? nullptr : (float*)workspace;
+            if (rows * dim * 3 * (int64_t)sizeof(T) < kRmsOnceBytes)
+                k_rms_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+            else
+                k_rms_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+        });
+        if (rows > 0 && !fits) {
+            if (dweight) {
+                const int64_t across = ceil_div(dim, kColumnThreads * (16 / (int64_t)sizeof(T)));
+                blocks = std::min<int64_t>(rows, std::max<int64_t>(1, kRmsGradBlocks / across));
+                a.dw = blocks == 1 ? (P*)dweight : nullptr;
+                a.sums = (float*)workspace;
+                k_rms_columns<<<dim3((uint32_t)across, (uint32_t)blocks), kColumnThreads, 0, s>>>(a);
+            }
+            k_rms_grad_wide<<<(uint32_t)std::min<int64_t>(kRmsBlocks, rows), kWideThreads, 0, s>>>(a);
+        }
+        if (dweight && !a.dw)  // without rows: zeros
+            k_rms_params<<<(uint32_t)ceil_div(dim, 64), 64 * kSlices, 0, s>>>((const float*)workspace, (int32_t)blocks, (int32_t)dim, (P*)dweight);
+    });
+    return launched("scd_rms_norm_grad");
+}

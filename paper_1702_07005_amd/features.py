@@ -1,4 +1,5 @@
-"""Operators of learned features: table lookup, layer norm, their gradients, and gradient clipping.
+"""Operators of learned features: table lookup, layer and root-mean-square norm, their gradients, gradient clipping, and
+the AdamW step.
 
 They serve models whose coordinates are rows of a learned table instead of one-hot columns: ids are
 looked up, the vectors normalised, a linear read-out is fitted on them by ``scd.Solver``, and the table is
@@ -22,6 +23,14 @@ refused unless gradients are off (``torch.no_grad()``).
     dx, dw, db = features.layer_norm_grad(dy, x, mean, rstd, weight)
     dtable = features.embed_grad(ids, dx, table.shape[0], scale=table.shape[1] ** 0.5)
     norm = features.clip_grads([dtable, dw, db], 1.0)
+
+With the root-mean-square norm, and with a step that clips on the way instead:
+
+    y, rstd, h = features.rms_norm(x, weight, residual)
+    dh, dw = features.rms_norm_grad(dy, h, rstd, weight)
+    params, grads = [table, weight], [dtable, dw]
+    state = features.adamw_state(params, bits=8)  # once
+    features.adamw(params, grads, state, step, lr=1e-3, norm=features.grad_norm(grads), max_norm=1.0)
 """
 from __future__ import annotations
 
@@ -52,12 +61,18 @@ def _elsewhere(tensor, stream, call, *args):
         if stream.device != tensor.device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {tensor.device}")
         context = torch.cuda.stream(stream)
-        for a in args:
-            for t in a if isinstance(a, (list, tuple)) else (a,):
-                if isinstance(t, torch.Tensor) and t.is_cuda:
-                    t.record_stream(stream)
+        _record(args, stream)
     with context:
         return call(*args)
+
+
+def _record(a, stream):
+    if isinstance(a, torch.Tensor):
+        if a.is_cuda:
+            a.record_stream(stream)
+    elif isinstance(a, (list, tuple)):
+        for t in a:
+            _record(t, stream)
 
 
 def embed(tokens, table, scale=1.0, out=None, dtype=None, stream=None):
@@ -114,6 +129,57 @@ def layer_norm_grad(grad, x, mean, rstd, weight=None, params=True, out=None, str
     return _elsewhere(x, stream, layer_norm_grad, grad, x, mean, rstd, weight, params, out)
 
 
+def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, sum_out=None, stream=None):
+    """``h * rstd * weight`` over the last dimension, with ``h = x + residual`` and ``rstd = 1 / sqrt(mean(h ** 2) + eps)``;
+    returns it with ``rstd`` (float32, one for each row) and ``h``, which ``rms_norm_grad`` takes.
+
+    The sum is rounded to ``x``'s type and normalised as it is kept; without a residual ``h`` is ``x``.  ``residual``: of
+    ``x``'s type and shape; ``weight``: [dim], of ``x``'s type or float32, or None.  ``out`` and ``sum_out`` (for ``h``) may be
+    ``x`` or ``residual``, but not the same."""
+    if stream is None:
+        d = _device()
+        result = _features.rms_norm(d, _stream(d), x, weight, residual, eps, out, sum_out, None)
+        if result is not None:
+            return result
+    return _elsewhere(x, stream, rms_norm, x, weight, residual, eps, out, sum_out)
+
+
+def rms_norm_8bit(x, weight=None, residual=None, eps=1e-6, group=None, out=None, sum_out=None, stream=None):
+    """``rms_norm`` with its result in 8 bits (``torch.float8_e4m3fn``) and scales; returns both with ``rstd`` and ``h``.
+
+    What the 8 bits stand for is their value times the scale: the largest magnitude of the row, or of each ``group`` (32, 64
+    or 128) columns, over 448.  ``scale``: float32, of ``x``'s leading shape, with a group [..., ceil(dim / group)].  The
+    result is rounded once, from 32 bits.  ``out``: of 8 bits, any row stride."""
+    if stream is None:
+        d = _device()
+        result = _features.rms_norm(d, _stream(d), x, weight, residual, eps, out, sum_out, _columns(group))
+        if result is not None:
+            return result
+    return _elsewhere(x, stream, rms_norm_8bit, x, weight, residual, eps, group, out, sum_out)
+
+
+def _columns(group):
+    if group is None:
+        return 0
+    if group not in (32, 64, 128):
+        raise ValueError("group must be None, 32, 64 or 128")
+    return int(group)
+
+
+def rms_norm_grad(grad, x, rstd, weight=None, residual_grad=None, params=True, out=None, stream=None):
+    """The gradients of ``rms_norm`` with respect to ``h`` (which is that of ``x`` and of ``residual`` alike) and ``weight``,
+    from the gradient of its output and the ``h`` (here ``x``) and ``rstd`` it returned.
+
+    ``residual_grad``, the gradient that reaches ``h`` another way, is added before the result is rounded.  The weight's has
+    its type (``x``'s where there is none) and is None with ``params=False``.  ``out`` may be any of the three matrices."""
+    if stream is None:
+        d = _device()
+        result = _features.rms_norm_grad(d, _stream(d), grad, x, rstd, weight, residual_grad, params, out)
+        if result is not None:
+            return result
+    return _elsewhere(x, stream, rms_norm_grad, grad, x, rstd, weight, residual_grad, params, out)
+
+
 def clip_grads(grads, max_norm, out=None, stream=None):
     """Scales the tensors of ``grads`` together so that their norm is at most ``max_norm``, in place or into the
     tensors of ``out`` (each of its gradient's type or float32).  Returns the norm before, a float32 tensor on
@@ -138,3 +204,53 @@ def _clip(grads, outs, max_norm, stream):
         if result is not None:
             return result
     return _elsewhere(grads[0] if grads else None, stream, _clip, grads, outs, max_norm, None)
+
+
+STATE_BLOCK = 256  # consecutive elements of a parameter whose states of 8 bits share a scale
+
+
+def adamw_state(params, bits=32):
+    """The states of ``params`` before the first step of ``adamw``, a tuple for each: the averages of the gradient and of its
+    square (float32), or with ``bits=8`` the average and the square root of the other (``torch.float8_e4m3fn``), then the
+    scales of both (float32, one for each 256 consecutive elements): what they stand for is their value times the scale."""
+    if bits not in (32, 8):
+        raise ValueError("bits must be 32 or 8")
+
+    def zeros(p):
+        if bits == 32:
+            return tuple(torch.zeros(p.shape, dtype=torch.float32, device=p.device) for _ in range(2))
+        blocks = (p.numel() + STATE_BLOCK - 1) // STATE_BLOCK
+        codes = [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for _ in range(2)]
+        return (*codes, *(torch.zeros(blocks, dtype=torch.float32, device=p.device) for _ in range(2)))
+
+    return [zeros(p) for p in params]
+
+
+def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, norm=None, max_norm=1.0, copies=None,
+          seed=0, stream=None):
+    """One AdamW step of all ``params`` together, in place, by ``grads`` and ``state`` (from ``adamw_state``; updated):
+
+        g = grad * min(1, max_norm / norm);  m = b1 * m + (1 - b1) * g;  v = b2 * v + (1 - b2) * g ** 2
+        param = param * (1 - lr * weight_decay) - lr * (m / (1 - b1 ** step)) / (sqrt(v / (1 - b2 ** step)) + eps)
+
+    ``params``: float32 with gradients of any type, or bfloat16 or float16 with gradients of that type or float32; tensors are
+    contiguous and on one device, and those that are written to share no memory with others of the call.  Parameters that
+    require gradients are updated under ``torch.no_grad()``.  ``step`` counts from 1.  It and ``lr`` may be tensors of one
+    element on the GPU (int64, float32), which a captured call reads at every replay.  ``weight_decay``: a number, or one for
+    each parameter.  ``norm``: that of all gradients, as ``grad_norm`` returns it, or None for no clipping.  ``copies``:
+    bfloat16 or float16 tensors (None for none) that receive the new float32 parameters.
+
+    States of 8 bits are rounded up or down at random, by a hash of ``seed``, ``step`` and the element's place, so that
+    small changes add up.  They cost 4 bytes of traffic an element instead of 16."""
+    listed = [a if a is None or isinstance(a, (list, tuple)) else list(a) for a in (params, grads, state, copies)]
+    decay = weight_decay if isinstance(weight_decay, (int, float, list, tuple)) else list(weight_decay)
+    _adamw(listed[0], listed[1], listed[2], step, lr, betas[0], betas[1], eps, decay, norm, max_norm, listed[3], seed, stream)
+
+
+def _adamw(params, grads, state, step, lr, beta1, beta2, eps, decay, norm, max_norm, copies, seed, stream):
+    if stream is None:
+        d = _device()
+        if _features.adamw(d, _stream(d), params, grads, state, step, lr, beta1, beta2, eps, decay, norm, max_norm, copies, seed) is not None:
+            return True
+    return _elsewhere(params[0] if params else None, stream, _adamw, params, grads, state, step, lr, beta1, beta2, eps, decay, norm, max_norm, copies,
+                      seed, None)
