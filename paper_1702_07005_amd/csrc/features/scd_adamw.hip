@@ -172,6 +172,20 @@ __device__ __forceinline__ float random_r(float x, float u) {
     return up ? b.high : b.low;
 }
 
+// The averages of a state in 8 bits.  Every product and sum rounds by itself, and scaled() below as a division does: a
+// state that lies at the border between up and down goes the same way wherever these formulas are computed in 32 bits.
+__device__ __forceinline__ void next_moments(const Common& c, float g, float m0, float r0, float& m, float& v) {
+#pragma clang fp contract(off)
+    m = c.b1 * m0 + c.a1 * g;
+    v = c.b2 * (r0 * r0) + c.a2 * (g * g);
+}
+
+// x / scale, rounded once: the product with the (rounded) inverse is off by two units at most, and the remainder corrects it.
+__device__ __forceinline__ float scaled(float x, float scale, float inverse) {
+    const float q = x * inverse;
+    return fmaf(fmaf(-q, scale, x), inverse, q);
+}
+
 // A block of a tensor, from the `at`-th element on, `n` of them: a wave.
 template <typename P, typename G>
 __device__ __forceinline__ void block_8(const Common& c, const Step& s, float keep, int64_t at, int32_t n) {
@@ -206,9 +220,7 @@ __device__ __forceinline__ void block_8(const Common& c, const Step& s, float ke
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         g[k] *= c.f;
-        m[k] = c.b1 * (m[k] * ms) + c.a1 * g[k];
-        const float r = v[k] * vs;
-        v[k] = c.b2 * (r * r) + c.a2 * (g[k] * g[k]);
+        next_moments(c, g[k], m[k] * ms, v[k] * vs, m[k], v[k]);
         p[k] = moved(c, keep, p[k], m[k], v[k]);
         v[k] = sqrtf(v[k]);
         most_m = fmaxf(most_m, fabsf(m[k]));
@@ -232,8 +244,8 @@ __device__ __forceinline__ void block_8(const Common& c, const Step& s, float ke
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const uint32_t word = murmur_fmix32((uint32_t)(from + k) ^ key);
-        m[k] = random_m(m[k] * im, ((float)(word & 0xFFFFu) + 0.5f) * 0x1p-16f);
-        v[k] = random_r(v[k] * iv, ((float)(word >> 16) + 0.5f) * 0x1p-16f);
+        m[k] = random_m(scaled(m[k], to_m, im), ((float)(word & 0xFFFFu) + 0.5f) * 0x1p-16f);
+        v[k] = random_r(scaled(v[k], to_v, iv), ((float)(word >> 16) + 0.5f) * 0x1p-16f);
     }
     mw = e4m3_pack4(m[0], m[1], m[2], m[3]);
     vw = e4m3_pack4(v[0], v[1], v[2], v[3]);

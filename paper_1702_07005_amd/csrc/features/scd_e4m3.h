@@ -14,9 +14,9 @@ constexpr float kTop = 448.0f;          // the largest value
 constexpr float kLeastNormal = 0x1p-6f;  // below it, values are multiples of 2^-9
 constexpr float kLeastScale = 0x1p-126f;
 
-// The scale of values up to `most`: they become at most 448 (1 + 2^-22), which rounds to 448.  Its least value keeps its
+// The scale of values up to `most`: they become at most 448 (1 + 2^-21), which rounds to 448.  Its least value keeps its
 // inverse finite.
-__device__ __forceinline__ float e4m3_scale(float most) { return fmaxf(most / kTop, kLeastScale); }
+__device__ __forceinline__ float e4m3_scale(float most) { return fmaxf(most * (1.0f / kTop), kLeastScale); }
 
 // To the nearest, ties to even.
 __device__ __forceinline__ uint32_t e4m3_pack4(float a, float b, float c, float d) {
