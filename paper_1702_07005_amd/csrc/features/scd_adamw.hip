@@ -8,7 +8,7 @@
 // run of consecutive chunks.  Launches do not depend on one another, and no element on another one but for the scales.
 //
 // In 8 bits (e4m3) a block of 256 elements has one scale for m and one for r = sqrt(v): the square root halves the range of
-// exponents that v would need.  A wave takes a block, four elements a lane.  States are rounded up or down at random: to the
+// exponents that v would need.  A wave takes two blocks, eight elements a lane.  States are rounded up or down at random: to the
 // nearest, v, which moves by a thousandth of itself in a step where half a step of its 8 bits is 6 to 12 %, would never move
 // again.  m goes up with the probability that keeps its mean, r with the one that keeps the mean of r^2; r > 0 never
 // becomes 0, where m over it would be without bound.  The random numbers are a hash of seed, step, tensor and element.
@@ -26,7 +26,7 @@ namespace {
 constexpr int kStepThreads = 256;
 constexpr int kSteps = 44;          // tensors a launch: the arguments stay below 4 KB
 constexpr int kStepBlocks = 2048;   // workgroups of a launch at most
-constexpr int kStateBlock = 256;    // elements that share a scale: a wave's
+constexpr int kStateBlock = 256;    // elements that share a scale
 constexpr int64_t kStepChunk = 4096;
 
 struct Step {
@@ -38,13 +38,14 @@ struct Step {
     float* vs;
     void* copy;
     int64_t n;
-    uint32_t first;  // number of chunks before this tensor's
     uint32_t place;  // in the call's list
     float decay;
     uint8_t pt, gt, ct, st;
+    uint32_t pad_;
 };
 struct StepArgs {
     Step s[kSteps];
+    uint32_t first[kSteps];  // number of chunks before each tensor's
     uint32_t count;
     uint32_t chunks;
     uint32_t chunk;  // elements of a chunk
@@ -52,13 +53,15 @@ struct StepArgs {
     const float* lr_dev;
     const int64_t* step_dev;
     const float* norm_dev;
+    int64_t step;
     double lr;
     double log_b1, log_b2;
     float b1, b2, a1, a2;  // a = 1 - b
     float eps, max_norm;
-    int64_t step;
+    float rate, root;  // where neither lr nor step are on the GPU
 };
 static_assert(sizeof(StepArgs) <= 4096, "kernel arguments");
+static_assert(kSteps <= 64, "a lane for each tensor");
 
 // What all elements of a launch share.
 struct Common {
@@ -81,30 +84,26 @@ __device__ __forceinline__ Common common_of(const StepArgs& a) {
         const float norm = *a.norm_dev;
         c.f = norm <= a.max_norm ? 1.0f : a.max_norm / norm;  // NaN: NaN
     }
-    const int64_t t = a.step_dev ? max(*a.step_dev, (int64_t)1) : a.step;
-    c.lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
-    // 1 - b^t without cancellation
-    c.rate = (float)(c.lr / -expm1((double)t * a.log_b1));
-    c.root = (float)(1.0 / sqrt(-expm1((double)t * a.log_b2)));
+    c.lr = a.lr;
+    c.rate = a.rate;
+    c.root = a.root;
+    int64_t t = a.step;
+    if (a.step_dev || a.lr_dev) {
+        if (a.step_dev) t = max(*a.step_dev, (int64_t)1);
+        if (a.lr_dev) c.lr = (double)*a.lr_dev;
+        // 1 - b^t without cancellation
+        c.rate = (float)(c.lr / -expm1((double)t * a.log_b1));
+        c.root = (float)(1.0 / sqrt(-expm1((double)t * a.log_b2)));
+    }
     c.key = murmur_fmix32(a.seed ^ murmur_fmix32((uint32_t)t));
     return c;
 }
 
-// The tensor that holds a chunk.
+// The tensor that holds a chunk: a lane looks at each.
 __device__ __forceinline__ uint32_t tensor_of(const StepArgs& a, uint32_t chunk) {
-    uint32_t lo = 0, hi = a.count;  // first[lo] <= chunk < first[hi]
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (a.s[mid].first <= chunk)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    return lo;
-}
-
-__device__ __forceinline__ float moved(const Common& c, float keep, float p, float m, float v) {
-    return p * keep - c.rate * m / (sqrtf(v) * c.root + c.eps);
+    const uint32_t lane = threadIdx.x % 64;
+    const uint64_t before = __ballot(lane < a.count && a.first[min(lane, (uint32_t)kSteps - 1)] <= chunk);
+    return (uint32_t)__builtin_popcountll(before) - 1;
 }
 
 template <int V>
@@ -128,7 +127,7 @@ __device__ __forceinline__ void step_32(const Common& c, const Step& s, float ke
         g[k] *= c.f;
         m[k] = c.b1 * m[k] + c.a1 * g[k];
         v[k] = c.b2 * v[k] + c.a2 * (g[k] * g[k]);
-        p[k] = moved(c, keep, p[k], m[k], v[k]);
+        p[k] = p[k] * keep - c.rate * m[k] / (sqrtf(v[k]) * c.root + c.eps);
     }
     store_vec((P*)s.p + i, p);
     store_vec((float*)s.m + i, m);
@@ -148,32 +147,12 @@ __device__ __forceinline__ void chunk_32(const Common& c, const Step& s, int64_t
     }
 }
 
-constexpr float kFinite = 0x1.fffffep127f;
+constexpr uint32_t kLargest = 0x7F7FFFFFu;  // bits of the largest finite number
+constexpr float kSmallRoot = 0x1p-96f;
 
-// A value x >= 0 between the neighbours low and high.
-struct Between {
-    float low, high;
-};
-__device__ __forceinline__ Between around(float x) {
-    const bool small = x < kLeastNormal;  // there the distance of neighbours is that of the binade above
-    const float shift = small ? kLeastNormal : 0.0f;
-    const uint32_t low = __float_as_uint(x + shift) & 0xFFF00000u;
-    return Between{__uint_as_float(low) - shift, __uint_as_float(low + 0x00100000u) - shift};
-}
-
-// u: uniform in (0, 1).  NaN and infinities come out as they are, and as NaN in 8 bits.
-__device__ __forceinline__ float random_m(float x, float u) {
-    const Between b = around(fabsf(x));
-    return copysignf(fabsf(x) - b.low > u * (b.high - b.low) ? b.high : b.low, x);
-}
-__device__ __forceinline__ float random_r(float x, float u) {
-    const Between b = around(x);
-    const bool up = (x - b.low) * (x + b.low) > u * (b.high - b.low) * (b.high + b.low) || (b.low == 0.0f && x > 0.0f);
-    return up ? b.high : b.low;
-}
-
-// The averages of a state in 8 bits.  Every product and sum rounds by itself, and scaled() below as a division does: a
-// state that lies at the border between up and down goes the same way wherever these formulas are computed in 32 bits.
+// The averages of a state in 8 bits.  Every product and sum rounds by itself, and scaled() and root() below as a division and
+// a square root do: a state that lies at the border between up and down goes the same way wherever these formulas are
+// computed in 32 bits.
 __device__ __forceinline__ void next_moments(const Common& c, float g, float m0, float r0, float& m, float& v) {
 #pragma clang fp contract(off)
     m = c.b1 * m0 + c.a1 * g;
@@ -186,87 +165,161 @@ __device__ __forceinline__ float scaled(float x, float scale, float inverse) {
     return fmaf(fmaf(-q, scale, x), inverse, q);
 }
 
-// A block of a tensor, from the `at`-th element on, `n` of them: a wave.
+// sqrt(v), rounded once, of 0 or v >= 2^-96.  The instruction's result s is a unit off at most; with its neighbour d below, s d
+// is the square of the point between them but for a quarter of a unit squared, so that v <= s d says that d is nearer.
+__device__ __forceinline__ float root(float v) {
+    const float s = __builtin_amdgcn_sqrtf(v);
+    const float down = __uint_as_float(__float_as_uint(s) - 1), up = __uint_as_float(__float_as_uint(s) + 1);
+    const float lower = fmaf(-down, s, v) <= 0.0f ? down : s;
+    return fmaf(-up, s, v) > 0.0f ? up : lower;
+}
+
+// The largest of the bits of numbers >= 0, whose order is that of the numbers, over 32 lanes; a NaN is above all.
+__device__ __forceinline__ uint32_t block_most(uint32_t x) {
+    const auto dpp = [](uint32_t y, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)y, decltype(ctrl)::value, 0xF, 0xF, false); };
+    x = max(x, dpp(x, Int<0xB1>{}));   // lane ^ 1
+    x = max(x, dpp(x, Int<0x4E>{}));   // lane ^ 2
+    x = max(x, dpp(x, Int<0x141>{}));  // other quad of 8
+    x = max(x, dpp(x, Int<0x140>{}));  // other half of 16
+    return max(x, (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F));  // lane ^ 16
+}
+
+// Four values in 8 bits, up or down with the random numbers of the words' low halves: the instruction adds its operand's 20
+// upper bits below the last bit that stays and cuts off.  It goes away from 0 where the fraction, of 20 bits, is above
+// (word mod 2^16 + 1/2) / 2^16.
+__device__ __forceinline__ uint32_t random_m4(const float* x, const uint32_t* word) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], 0xFFFF7000u - (word[0] << 16), w, 0);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], 0xFFFF7000u - (word[1] << 16), w, 1);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], 0xFFFF7000u - (word[2] << 16), w, 2);
+    return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x[3], 0xFFFF7000u - (word[3] << 16), w, 3);
+}
+
+// The same with the words' high halves and the probabilities that keep the mean of the square: cut off first, then one further
+// where (x^2 - low^2) / (high^2 - low^2) is above the random number.  x is 0 or at least the least value.  Above the
+// largest value there is NaN, which no comparison chooses.
+__device__ __forceinline__ uint32_t random_r4(const float* x, const uint32_t* word) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], 0, w, 0);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], 0, w, 1);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], 0, w, 2);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[3], 0, w, 3);
+    const int above = w + 0x01010101;
+    const auto l01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), l23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    const auto h01 = __builtin_amdgcn_cvt_pk_f32_fp8(above, false), h23 = __builtin_amdgcn_cvt_pk_f32_fp8(above, true);
+    const float low[4] = {l01[0], l01[1], l23[0], l23[1]}, high[4] = {h01[0], h01[1], h23[0], h23[1]};
+    uint32_t out = (uint32_t)w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float u = fmaf((float)(word[k] >> 16), 0x1p-16f, 0x1p-17f);
+        const bool up = (x[k] - low[k]) * (x[k] + low[k]) > (high[k] - low[k]) * u * (high[k] + low[k]);
+        out += up ? 1u << (8 * k) : 0u;
+    }
+    return out;
+}
+
+// Two blocks of a tensor, from the `at`-th element on, `n` elements of them: a wave.
 template <typename P, typename G>
-__device__ __forceinline__ void block_8(const Common& c, const Step& s, float keep, int64_t at, int32_t n) {
-    constexpr int V = 4;
+__device__ __forceinline__ void blocks_8(const Common& c, const Step& s, float keep, int64_t at, int32_t n) {
+    constexpr int V = 8;
     const int32_t lane = threadIdx.x % 64, i = lane * V;
-    const int64_t from = at + i, block = at / kStateBlock;
-    const bool whole = i + V <= n;
+    const int64_t from = at + i, block = from / kStateBlock;
+    const bool whole = i + V <= n, there = i / kStateBlock * kStateBlock < n;
     float p[V] = {}, g[V] = {};
-    uint32_t mw = 0, vw = 0;
-    const uint8_t* const mq = (const uint8_t*)s.m + from;
-    const uint8_t* const vq = (const uint8_t*)s.v + from;
+    uint32_t mw[2] = {}, vw[2] = {};
+    uint8_t* const mq = (uint8_t*)s.m + from;
+    uint8_t* const vq = (uint8_t*)s.v + from;
     if (whole) {
         load_vec((const P*)s.p + from, p);
         load_vec((const G*)s.g + from, g);
-        __builtin_memcpy(&mw, mq, 4);
-        __builtin_memcpy(&vw, vq, 4);
+        __builtin_memcpy(mw, mq, 8);
+        __builtin_memcpy(vw, vq, 8);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
             if (i + k < n) {
                 p[k] = (float)((const P*)s.p)[from + k];
                 g[k] = (float)((const G*)s.g)[from + k];
-                mw |= (uint32_t)mq[k] << (8 * k);
-                vw |= (uint32_t)vq[k] << (8 * k);
+                mw[k / 4] |= (uint32_t)mq[k] << (8 * (k % 4));
+                vw[k / 4] |= (uint32_t)vq[k] << (8 * (k % 4));
             }
     }
-    const float ms = s.ms[block], vs = s.vs[block];
-    const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mw, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mw, true);
-    const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(vw, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(vw, true);
-    float m[V] = {m01[0], m01[1], m23[0], m23[1]}, v[V] = {v01[0], v01[1], v23[0], v23[1]};
-    float most_m = 0.0f, most_v = 0.0f;
+    const float ms = there ? s.ms[block] : 0.0f, vs = there ? s.vs[block] : 0.0f;
+    float m[V], v[V], r[V];
+#pragma unroll
+    for (int k = 0; k < V / 4; ++k) {
+        const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mw[k], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mw[k], true);
+        const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(vw[k], false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(vw[k], true);
+        m[4 * k] = m01[0], m[4 * k + 1] = m01[1], m[4 * k + 2] = m23[0], m[4 * k + 3] = m23[1];
+        v[4 * k] = v01[0], v[4 * k + 1] = v01[1], v[4 * k + 2] = v23[0], v[4 * k + 3] = v23[1];
+    }
+    uint32_t most_m = 0, most_v = 0, least = 0xFFFFFFFFu;  // `least`: below the bits of v > 0
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        g[k] *= c.f;
-        next_moments(c, g[k], m[k] * ms, v[k] * vs, m[k], v[k]);
-        p[k] = moved(c, keep, p[k], m[k], v[k]);
-        v[k] = sqrtf(v[k]);
-        most_m = fmaxf(most_m, fabsf(m[k]));
-        most_v = fmaxf(most_v, v[k]);
+        next_moments(c, g[k] * c.f, m[k] * ms, v[k] * vs, m[k], v[k]);
+        most_m = max(most_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+        most_v = max(most_v, __float_as_uint(v[k]));
+        least = min(least, __float_as_uint(v[k]) - 1);
     }
-    most_m = group_max<64>(most_m, 64);
-    most_v = group_max<64>(most_v, 64);
-    if (!(fmaxf(most_m, most_v) <= kFinite)) {  // rare: infinite ones leave the others their scale
-        most_m = most_v = 0.0f;
+    if (least < __float_as_uint(kSmallRoot)) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) r[k] = sqrtf(v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) r[k] = root(v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) p[k] = p[k] * keep - c.rate * m[k] * __builtin_amdgcn_rcpf(r[k] * c.root + c.eps);
+    most_m = block_most(most_m);
+    most_v = block_most(most_v);
+    const bool odd = max(most_m, most_v) > kLargest;
+    if (odd) {  // infinite values and NaN leave the others their scale
+        most_m = most_v = 0;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            most_m = fmaxf(most_m, fabsf(m[k]) <= kFinite ? fabsf(m[k]) : 0.0f);
-            most_v = fmaxf(most_v, v[k] <= kFinite ? v[k] : 0.0f);
+            const uint32_t x = __float_as_uint(m[k]) & 0x7FFFFFFFu, y = __float_as_uint(v[k]);
+            most_m = max(most_m, x <= kLargest ? x : 0u);
+            most_v = max(most_v, y <= kLargest ? y : 0u);
         }
-        most_m = group_max<64>(most_m, 64);
-        most_v = group_max<64>(most_v, 64);
+        most_m = block_most(most_m);
+        most_v = block_most(most_v);
     }
-    const float to_m = e4m3_scale(most_m), to_v = e4m3_scale(most_v);
+    const float to_m = e4m3_scale(__uint_as_float(most_m)), to_v = e4m3_scale(sqrtf(__uint_as_float(most_v)));
     const float im = 1.0f / to_m, iv = 1.0f / to_v;
     const uint32_t key = murmur_fmix32(c.key + s.place) + (uint32_t)((uint64_t)at >> 32);
+    uint32_t word[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        const uint32_t word = murmur_fmix32((uint32_t)(from + k) ^ key);
-        m[k] = random_m(scaled(m[k], to_m, im), ((float)(word & 0xFFFFu) + 0.5f) * 0x1p-16f);
-        v[k] = random_r(scaled(v[k], to_v, iv), ((float)(word >> 16) + 0.5f) * 0x1p-16f);
+        word[k] = murmur_fmix32((uint32_t)(from + k) ^ key);
+        m[k] = scaled(m[k], to_m, im);
+        r[k] = r[k] == 0.0f ? 0.0f : fmaxf(scaled(r[k], to_v, iv), kLeast);
     }
-    mw = e4m3_pack4(m[0], m[1], m[2], m[3]);
-    vw = e4m3_pack4(v[0], v[1], v[2], v[3]);
-    if (lane == 0) {
+#pragma unroll
+    for (int k = 0; k < V / 4; ++k) {
+        mw[k] = random_m4(m + 4 * k, word + 4 * k);
+        vw[k] = random_r4(r + 4 * k, word + 4 * k);
+    }
+    if (odd) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (__float_as_uint(v[k]) > kLargest) vw[k / 4] |= 0x7Fu << (8 * (k % 4));
+    }
+    if (there && i % kStateBlock == 0) {
         s.ms[block] = to_m;
         s.vs[block] = to_v;
     }
-    uint8_t* const mo = (uint8_t*)s.m + from;
-    uint8_t* const vo = (uint8_t*)s.v + from;
     if (whole) {
         store_vec((P*)s.p + from, p);
-        __builtin_memcpy(mo, &mw, 4);
-        __builtin_memcpy(vo, &vw, 4);
+        __builtin_memcpy(mq, mw, 8);
+        __builtin_memcpy(vq, vw, 8);
         if (s.copy) store_copy(s.copy, s.ct, from, p);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
             if (i + k < n) {
                 ((P*)s.p)[from + k] = (P)p[k];
-                mo[k] = (uint8_t)(mw >> (8 * k));
-                vo[k] = (uint8_t)(vw >> (8 * k));
+                mq[k] = (uint8_t)(mw[k / 4] >> (8 * (k % 4)));
+                vq[k] = (uint8_t)(vw[k / 4] >> (8 * (k % 4)));
                 if (s.copy) {
                     const float one[1] = {p[k]};
                     store_copy(s.copy, s.ct, from + k, one);
@@ -277,9 +330,9 @@ __device__ __forceinline__ void block_8(const Common& c, const Step& s, float ke
 
 template <typename P, typename G>
 __device__ __forceinline__ void chunk_8(const Common& c, const Step& s, int64_t at, int32_t n) {
+    constexpr int32_t kWave = 2 * kStateBlock;
     const float keep = (float)(1.0 - c.lr * (double)s.decay);
-    for (int32_t b = threadIdx.x / 64 * kStateBlock; b < n; b += kStepThreads / 64 * kStateBlock)
-        block_8<P, G>(c, s, keep, at + b, min(kStateBlock, n - b));
+    for (int32_t b = threadIdx.x / 64 * kWave; b < n; b += kStepThreads / 64 * kWave) blocks_8<P, G>(c, s, keep, at + b, min(kWave, n - b));
 }
 
 template <typename P, typename G>
@@ -296,9 +349,9 @@ __global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs a) {
     const uint32_t c1 = (uint32_t)((uint64_t)a.chunks * (blockIdx.x + 1) / gridDim.x);
     uint32_t k = tensor_of(a, c0);
     for (uint32_t chunk = c0; chunk < c1; ++chunk) {
-        while (k + 1 < a.count && a.s[k + 1].first <= chunk) ++k;
+        while (k + 1 < a.count && a.first[k + 1] <= chunk) ++k;
         const Step& s = a.s[k];
-        const int64_t at = (int64_t)(chunk - s.first) * a.chunk;
+        const int64_t at = (int64_t)(chunk - a.first[k]) * a.chunk;
         const int32_t n = (int32_t)min((int64_t)a.chunk, s.n - at);
         if (s.pt == SCD_F32) {
             if (s.gt == SCD_F32)
@@ -353,7 +406,7 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
     if (total == 0) return SCD_OK;
     StepArgs a;
     // Small chunks where whole ones would leave CUs idle.
-    a.chunk = (uint32_t)(total < kStepChunk * kStepBlocks ? kStepChunk / 4 : kStepChunk);
+    a.chunk = (uint32_t)(total < kStepChunk * kStepBlocks ? kStepChunk / 2 : kStepChunk);
     a.seed = o.seed;
     a.lr_dev = o.lr_dev;
     a.step_dev = o.step_dev;
@@ -368,6 +421,8 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
     a.eps = (float)o.eps;
     a.max_norm = o.max_norm;
     a.step = o.step;
+    a.rate = (float)(o.lr / -std::expm1((double)o.step * a.log_b1));
+    a.root = (float)(1.0 / std::sqrt(-std::expm1((double)o.step * a.log_b2)));
     hipStream_t s = (hipStream_t)stream;
     for (int64_t i = 0; i < count;) {
         a.count = 0;
@@ -375,8 +430,9 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
         for (; i < count && a.count < kSteps; ++i) {
             const scd_adamw_span_t& t = spans[i];
             if (t.n == 0) continue;
-            a.s[a.count++] = Step{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, a.chunks, (uint32_t)i, t.weight_decay, (uint8_t)t.param_type,
-                                  (uint8_t)t.grad_type, (uint8_t)t.copy_type, (uint8_t)t.state_type};
+            a.first[a.count] = a.chunks;
+            a.s[a.count++] = Step{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, (uint32_t)i, t.weight_decay, (uint8_t)t.param_type,
+                                  (uint8_t)t.grad_type, (uint8_t)t.copy_type, (uint8_t)t.state_type, 0};
             a.chunks += (uint32_t)ceil_div(t.n, (int64_t)a.chunk);
         }
         if (a.count) k_adamw<<<std::min<uint32_t>(kStepBlocks, a.chunks), kStepThreads, 0, s>>>(a);

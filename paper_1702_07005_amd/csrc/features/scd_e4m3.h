@@ -11,7 +11,7 @@ namespace scd {
 namespace feat {
 
 constexpr float kTop = 448.0f;          // the largest value
-constexpr float kLeastNormal = 0x1p-6f;  // below it, values are multiples of 2^-9
+constexpr float kLeast = 0x1p-9f;        // the least above 0
 constexpr float kLeastScale = 0x1p-126f;
 
 // The scale of values up to `most`: they become at most 448 (1 + 2^-21), which rounds to 448.  Its least value keeps its

@@ -182,6 +182,9 @@ def adamw(p, grad, state, step, lr, betas, eps, decay, norm=None, max_norm=1.0, 
         per = scale.repeat_interleave(BLOCK)[:x.numel()]
         z = x.reshape(-1).abs() / per
         e_z = SLACK * (e.reshape(-1) / per + z * (e_scale.repeat_interleave(BLOCK)[:x.numel()] / per + 3 * U))
+        # what lies between two neighbours is compared in 20 bits: nothing is lost from 2^-6 on, where a value has as many below
+        # its first four; below, bits under 2^-9 / 2^20 are
+        e_z = e_z + torch.where(z < 2.0 ** -6, 2.0 ** -29, 0.0)
         least, most = to((z - e_z).clamp(min=0.0), u), to(z + e_z, u)
         out[name] = (least.view(p.shape), most.view(p.shape), torch.sign(x))
         out[name + "_scale"] = (scale, e_scale)
