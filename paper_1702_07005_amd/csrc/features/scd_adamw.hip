@@ -25,9 +25,12 @@ namespace {
 
 constexpr int kStepThreads = 256;
 constexpr int kSteps = 44;          // tensors a launch: the arguments stay below 4 KB
-constexpr int kStepBlocks = 2048;   // workgroups of a launch at most
 constexpr int kStateBlock = 256;    // elements that share a scale
-constexpr int64_t kStepChunk = 4096;
+constexpr int64_t kStepChunk = 1024;   // elements of a workgroup, 32 bits
+constexpr int64_t kStepChunk8 = 2048;  // and 8
+// Elements of a call at most: a launch has fewer than 2^32 threads, though every tensor's last chunk may be short.
+constexpr int64_t kStepMost = (0xFFFFFF - kSteps) * kStepChunk;
+constexpr int64_t kStepOnce = int64_t(256) << 20;
 
 struct Step {
     void* p;
@@ -106,22 +109,44 @@ __device__ __forceinline__ uint32_t tensor_of(const StepArgs& a, uint32_t chunk)
     return (uint32_t)__builtin_popcountll(before) - 1;
 }
 
-template <int V>
+template <bool ONCE, int V>
 __device__ __forceinline__ void store_copy(void* copy, int32_t type, int64_t i, const float (&p)[V]) {
     if (type == SCD_BF16)
-        store_vec((bf16*)copy + i, p);
+        put_vec<ONCE>((bf16*)copy + i, p);
     else
-        store_vec((f16*)copy + i, p);
+        put_vec<ONCE>((f16*)copy + i, p);
+}
+
+template <bool ONCE, int V, typename T>
+__device__ __forceinline__ void fetch_vec(const T* p, float (&o)[V]) {
+    widen(fetch_raw<V, ONCE>(p), o);
+}
+
+// Eight values of 8 bits.
+typedef uint32_t Eight __attribute__((ext_vector_type(2), aligned(1)));
+template <bool ONCE>
+__device__ __forceinline__ void fetch_8(uint32_t (&w)[2], const uint8_t* p) {
+    const Eight x = ONCE ? __builtin_nontemporal_load((const Eight*)p) : *(const Eight*)p;
+    w[0] = x[0];
+    w[1] = x[1];
+}
+template <bool ONCE>
+__device__ __forceinline__ void put_8(uint8_t* p, const uint32_t (&w)[2]) {
+    const Eight x = {w[0], w[1]};
+    if (ONCE)
+        __builtin_nontemporal_store(x, (Eight*)p);
+    else
+        *(Eight*)p = x;
 }
 
 // V elements from the i-th on, states in 32 bits.
-template <int V, typename P, typename G>
+template <bool ONCE, int V, typename P, typename G>
 __device__ __forceinline__ void step_32(const Common& c, const Step& s, float keep, int64_t i) {
     float p[V], g[V], m[V], v[V];
-    load_vec((const P*)s.p + i, p);
-    load_vec((const G*)s.g + i, g);
-    load_vec((const float*)s.m + i, m);
-    load_vec((const float*)s.v + i, v);
+    fetch_vec<ONCE>((const P*)s.p + i, p);
+    fetch_vec<ONCE>((const G*)s.g + i, g);
+    fetch_vec<ONCE>((const float*)s.m + i, m);
+    fetch_vec<ONCE>((const float*)s.v + i, v);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         g[k] *= c.f;
@@ -129,20 +154,20 @@ __device__ __forceinline__ void step_32(const Common& c, const Step& s, float ke
         v[k] = c.b2 * v[k] + c.a2 * (g[k] * g[k]);
         p[k] = p[k] * keep - c.rate * m[k] / (sqrtf(v[k]) * c.root + c.eps);
     }
-    store_vec((P*)s.p + i, p);
-    store_vec((float*)s.m + i, m);
-    store_vec((float*)s.v + i, v);
-    if (s.copy) store_copy(s.copy, s.ct, i, p);
+    put_vec<ONCE>((P*)s.p + i, p);
+    put_vec<ONCE>((float*)s.m + i, m);
+    put_vec<ONCE>((float*)s.v + i, v);
+    if (s.copy) store_copy<ONCE>(s.copy, s.ct, i, p);
 }
 
-template <typename P, typename G>
+template <bool ONCE, typename P, typename G>
 __device__ __forceinline__ void chunk_32(const Common& c, const Step& s, int64_t at, int32_t n) {
     const float keep = (float)(1.0 - c.lr * (double)s.decay);
     for (int32_t i = threadIdx.x * 4; i < n; i += kStepThreads * 4) {
         if (i + 4 <= n) {
-            step_32<4, P, G>(c, s, keep, at + i);
+            step_32<ONCE, 4, P, G>(c, s, keep, at + i);
         } else {
-            for (int32_t k = i; k < n; ++k) step_32<1, P, G>(c, s, keep, at + k);
+            for (int32_t k = i; k < n; ++k) step_32<false, 1, P, G>(c, s, keep, at + k);
         }
     }
 }
@@ -157,6 +182,12 @@ __device__ __forceinline__ void next_moments(const Common& c, float g, float m0,
 #pragma clang fp contract(off)
     m = c.b1 * m0 + c.a1 * g;
     v = c.b2 * (r0 * r0) + c.a2 * (g * g);
+}
+
+// 1 / scale, rounded once: the instruction's result is a unit off at most, and the remainder corrects it.
+__device__ __forceinline__ float inverse(float scale) {
+    const float q = __builtin_amdgcn_rcpf(scale);
+    return fmaf(fmaf(-q, scale, 1.0f), q, q);
 }
 
 // x / scale, rounded once: the product with the (rounded) inverse is off by two units at most, and the remainder corrects it.
@@ -184,15 +215,18 @@ __device__ __forceinline__ uint32_t block_most(uint32_t x) {
     return max(x, (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F));  // lane ^ 16
 }
 
+// What the conversion adds for a word: 2^16 - 1 less its low half, and 7 sixteenths.
+__device__ __forceinline__ uint32_t random_bits(uint32_t word) { return (~word << 16) | 0x7000u; }
+
 // Four values in 8 bits, up or down with the random numbers of the words' low halves: the instruction adds its operand's 20
 // upper bits below the last bit that stays and cuts off.  It goes away from 0 where the fraction, of 20 bits, is above
 // (word mod 2^16 + 1/2) / 2^16.
 __device__ __forceinline__ uint32_t random_m4(const float* x, const uint32_t* word) {
     int w = 0;
-    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], 0xFFFF7000u - (word[0] << 16), w, 0);
-    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], 0xFFFF7000u - (word[1] << 16), w, 1);
-    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], 0xFFFF7000u - (word[2] << 16), w, 2);
-    return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x[3], 0xFFFF7000u - (word[3] << 16), w, 3);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], random_bits(word[0]), w, 0);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], random_bits(word[1]), w, 1);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], random_bits(word[2]), w, 2);
+    return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x[3], random_bits(word[3]), w, 3);
 }
 
 // The same with the words' high halves and the probabilities that keep the mean of the square: cut off first, then one further
@@ -219,21 +253,21 @@ __device__ __forceinline__ uint32_t random_r4(const float* x, const uint32_t* wo
 }
 
 // Two blocks of a tensor, from the `at`-th element on, `n` elements of them: a wave.
-template <typename P, typename G>
+template <bool ONCE, typename P, typename G>
 __device__ __forceinline__ void blocks_8(const Common& c, const Step& s, float keep, int64_t at, int32_t n) {
     constexpr int V = 8;
     const int32_t lane = threadIdx.x % 64, i = lane * V;
     const int64_t from = at + i, block = from / kStateBlock;
     const bool whole = i + V <= n, there = i / kStateBlock * kStateBlock < n;
     float p[V] = {}, g[V] = {};
-    uint32_t mw[2] = {}, vw[2] = {};
+    uint32_t mw[2] = {}, rw[2] = {};
     uint8_t* const mq = (uint8_t*)s.m + from;
-    uint8_t* const vq = (uint8_t*)s.v + from;
+    uint8_t* const rq = (uint8_t*)s.v + from;
     if (whole) {
-        load_vec((const P*)s.p + from, p);
-        load_vec((const G*)s.g + from, g);
-        __builtin_memcpy(mw, mq, 8);
-        __builtin_memcpy(vw, vq, 8);
+        fetch_vec<ONCE>((const P*)s.p + from, p);
+        fetch_vec<ONCE>((const G*)s.g + from, g);
+        fetch_8<ONCE>(mw, mq);
+        fetch_8<ONCE>(rw, rq);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -241,137 +275,127 @@ __device__ __forceinline__ void blocks_8(const Common& c, const Step& s, float k
                 p[k] = (float)((const P*)s.p)[from + k];
                 g[k] = (float)((const G*)s.g)[from + k];
                 mw[k / 4] |= (uint32_t)mq[k] << (8 * (k % 4));
-                vw[k / 4] |= (uint32_t)vq[k] << (8 * (k % 4));
+                rw[k / 4] |= (uint32_t)rq[k] << (8 * (k % 4));
             }
     }
-    const float ms = there ? s.ms[block] : 0.0f, vs = there ? s.vs[block] : 0.0f;
-    float m[V], v[V], r[V];
+    const float ms = there ? s.ms[block] : 0.0f, rs = there ? s.vs[block] : 0.0f;
+    float m[V], r[V];
 #pragma unroll
     for (int k = 0; k < V / 4; ++k) {
         const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mw[k], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mw[k], true);
-        const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(vw[k], false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(vw[k], true);
+        const auto r01 = __builtin_amdgcn_cvt_pk_f32_fp8(rw[k], false), r23 = __builtin_amdgcn_cvt_pk_f32_fp8(rw[k], true);
         m[4 * k] = m01[0], m[4 * k + 1] = m01[1], m[4 * k + 2] = m23[0], m[4 * k + 3] = m23[1];
-        v[4 * k] = v01[0], v[4 * k + 1] = v01[1], v[4 * k + 2] = v23[0], v[4 * k + 3] = v23[1];
+        r[4 * k] = r01[0], r[4 * k + 1] = r01[1], r[4 * k + 2] = r23[0], r[4 * k + 3] = r23[1];
     }
-    uint32_t most_m = 0, most_v = 0, least = 0xFFFFFFFFu;  // `least`: below the bits of v > 0
+    uint32_t least = 0xFFFFFFFFu;  // below the bits of v > 0
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        next_moments(c, g[k] * c.f, m[k] * ms, v[k] * vs, m[k], v[k]);
-        most_m = max(most_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
-        most_v = max(most_v, __float_as_uint(v[k]));
-        least = min(least, __float_as_uint(v[k]) - 1);
+        next_moments(c, g[k] * c.f, m[k] * ms, r[k] * rs, m[k], r[k]);
+        least = min(least, __float_as_uint(r[k]) - 1);
     }
     if (least < __float_as_uint(kSmallRoot)) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) r[k] = sqrtf(v[k]);
+        for (int k = 0; k < V; ++k) r[k] = sqrtf(r[k]);
     } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k) r[k] = root(v[k]);
+        for (int k = 0; k < V; ++k) r[k] = root(r[k]);
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) p[k] = p[k] * keep - c.rate * m[k] * __builtin_amdgcn_rcpf(r[k] * c.root + c.eps);
-    most_m = block_most(most_m);
-    most_v = block_most(most_v);
-    const bool odd = max(most_m, most_v) > kLargest;
-    if (odd) {  // infinite values and NaN leave the others their scale
-        most_m = most_v = 0;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const uint32_t x = __float_as_uint(m[k]) & 0x7FFFFFFFu, y = __float_as_uint(v[k]);
-            most_m = max(most_m, x <= kLargest ? x : 0u);
-            most_v = max(most_v, y <= kLargest ? y : 0u);
-        }
-        most_m = block_most(most_m);
-        most_v = block_most(most_v);
-    }
-    const float to_m = e4m3_scale(__uint_as_float(most_m)), to_v = e4m3_scale(sqrtf(__uint_as_float(most_v)));
-    const float im = 1.0f / to_m, iv = 1.0f / to_v;
-    const uint32_t key = murmur_fmix32(c.key + s.place) + (uint32_t)((uint64_t)at >> 32);
-    uint32_t word[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-        word[k] = murmur_fmix32((uint32_t)(from + k) ^ key);
-        m[k] = scaled(m[k], to_m, im);
-        r[k] = r[k] == 0.0f ? 0.0f : fmaxf(scaled(r[k], to_v, iv), kLeast);
-    }
-#pragma unroll
-    for (int k = 0; k < V / 4; ++k) {
-        mw[k] = random_m4(m + 4 * k, word + 4 * k);
-        vw[k] = random_r4(r + 4 * k, word + 4 * k);
-    }
-    if (odd) {
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (__float_as_uint(v[k]) > kLargest) vw[k / 4] |= 0x7Fu << (8 * (k % 4));
-    }
-    if (there && i % kStateBlock == 0) {
-        s.ms[block] = to_m;
-        s.vs[block] = to_v;
-    }
     if (whole) {
-        store_vec((P*)s.p + from, p);
-        __builtin_memcpy(mq, mw, 8);
-        __builtin_memcpy(vq, vw, 8);
-        if (s.copy) store_copy(s.copy, s.ct, from, p);
+        put_vec<ONCE>((P*)s.p + from, p);
+        if (s.copy) store_copy<ONCE>(s.copy, s.ct, from, p);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
             if (i + k < n) {
-                ((P*)s.p)[from + k] = (P)p[k];
+                const float one[1] = {p[k]};
+                store_vec((P*)s.p + from + k, one);
+                if (s.copy) store_copy<false>(s.copy, s.ct, from + k, one);
+            }
+    }
+    uint32_t most_m = 0, most_r = 0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        most_m = max(most_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+        most_r = max(most_r, __float_as_uint(r[k]));
+    }
+    most_m = block_most(most_m);
+    most_r = block_most(most_r);
+    uint32_t lost[V / 4] = {};
+    if (__ballot(max(most_m, most_r) > kLargest)) {  // infinite values and NaN leave the others their scale
+        most_m = most_r = 0;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const uint32_t x = __float_as_uint(m[k]) & 0x7FFFFFFFu, y = __float_as_uint(r[k]);
+            most_m = max(most_m, x <= kLargest ? x : 0u);
+            most_r = max(most_r, y <= kLargest ? y : 0u);
+            if (y > kLargest) lost[k / 4] |= 0x7Fu << (8 * (k % 4));
+        }
+        most_m = block_most(most_m);
+        most_r = block_most(most_r);
+    }
+    const float to_m = e4m3_scale(__uint_as_float(most_m)), to_r = e4m3_scale(__uint_as_float(most_r));
+    const float im = inverse(to_m), ir = inverse(to_r);
+    const uint32_t key = murmur_fmix32(c.key + s.place) + (uint32_t)((uint64_t)at >> 32);
+#pragma unroll
+    for (int k = 0; k < V / 4; ++k) {
+        uint32_t word[4];
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {
+            float& x = r[4 * k + l];
+            word[l] = murmur_fmix32((uint32_t)(from + 4 * k + l) ^ key);
+            m[4 * k + l] = scaled(m[4 * k + l], to_m, im);
+            x = x == 0.0f ? 0.0f : fmaxf(scaled(x, to_r, ir), kLeast);
+        }
+        mw[k] = random_m4(m + 4 * k, word);
+        rw[k] = random_r4(r + 4 * k, word) | lost[k];
+    }
+    if (there && i % kStateBlock == 0) {
+        s.ms[block] = to_m;
+        s.vs[block] = to_r;
+    }
+    if (whole) {
+        put_8<ONCE>(mq, mw);
+        put_8<ONCE>(rq, rw);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (i + k < n) {
                 mq[k] = (uint8_t)(mw[k / 4] >> (8 * (k % 4)));
-                vq[k] = (uint8_t)(vw[k / 4] >> (8 * (k % 4)));
-                if (s.copy) {
-                    const float one[1] = {p[k]};
-                    store_copy(s.copy, s.ct, from + k, one);
-                }
+                rq[k] = (uint8_t)(rw[k / 4] >> (8 * (k % 4)));
             }
     }
 }
 
-template <typename P, typename G>
+template <bool ONCE, typename P, typename G>
 __device__ __forceinline__ void chunk_8(const Common& c, const Step& s, int64_t at, int32_t n) {
     constexpr int32_t kWave = 2 * kStateBlock;
     const float keep = (float)(1.0 - c.lr * (double)s.decay);
-    for (int32_t b = threadIdx.x / 64 * kWave; b < n; b += kStepThreads / 64 * kWave) blocks_8<P, G>(c, s, keep, at + b, min(kWave, n - b));
+    for (int32_t b = threadIdx.x / 64 * kWave; b < n; b += kStepThreads / 64 * kWave) blocks_8<ONCE, P, G>(c, s, keep, at + b, min(kWave, n - b));
 }
 
-template <typename P, typename G>
-__device__ __forceinline__ void chunk_step(const Common& c, const Step& s, int64_t at, int32_t n) {
-    if (s.st == SCD_F32)
-        chunk_32<P, G>(c, s, at, n);
-    else
-        chunk_8<P, G>(c, s, at, n);
-}
-
+// EIGHT: the tensors of a launch have states in 8 bits.  A workgroup for each chunk, in order: what runs at a time lies close
+// together in memory.
+template <bool EIGHT, bool ONCE>
 __global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs a) {
     const Common c = common_of(a);
-    const uint32_t c0 = (uint32_t)((uint64_t)a.chunks * blockIdx.x / gridDim.x);
-    const uint32_t c1 = (uint32_t)((uint64_t)a.chunks * (blockIdx.x + 1) / gridDim.x);
-    uint32_t k = tensor_of(a, c0);
-    for (uint32_t chunk = c0; chunk < c1; ++chunk) {
-        while (k + 1 < a.count && a.first[k + 1] <= chunk) ++k;
-        const Step& s = a.s[k];
-        const int64_t at = (int64_t)(chunk - a.first[k]) * a.chunk;
-        const int32_t n = (int32_t)min((int64_t)a.chunk, s.n - at);
-        if (s.pt == SCD_F32) {
-            if (s.gt == SCD_F32)
-                chunk_step<float, float>(c, s, at, n);
-            else if (s.gt == SCD_BF16)
-                chunk_step<float, bf16>(c, s, at, n);
-            else
-                chunk_step<float, f16>(c, s, at, n);
-        } else if (s.pt == SCD_BF16) {
-            if (s.gt == SCD_F32)
-                chunk_step<bf16, float>(c, s, at, n);
-            else
-                chunk_step<bf16, bf16>(c, s, at, n);
-        } else {
-            if (s.gt == SCD_F32)
-                chunk_step<f16, float>(c, s, at, n);
-            else
-                chunk_step<f16, f16>(c, s, at, n);
-        }
-    }
+    const uint32_t chunk = blockIdx.x, k = tensor_of(a, chunk);
+    const Step& s = a.s[k];
+    const int64_t at = (int64_t)(chunk - a.first[k]) * a.chunk;
+    const int32_t n = (int32_t)min((int64_t)a.chunk, s.n - at);
+    const auto step = [&](auto p, auto g) {
+        if constexpr (EIGHT)
+            chunk_8<ONCE, decltype(p), decltype(g)>(c, s, at, n);
+        else
+            chunk_32<ONCE, decltype(p), decltype(g)>(c, s, at, n);
+    };
+    if (s.pt == SCD_F32)
+        s.gt == SCD_F32 ? step(float{}, float{}) : s.gt == SCD_BF16 ? step(float{}, bf16{}) : step(float{}, f16{});
+    else if (s.pt == SCD_BF16)
+        s.gt == SCD_F32 ? step(bf16{}, float{}) : step(bf16{}, bf16{});
+    else
+        s.gt == SCD_F32 ? step(f16{}, float{}) : step(f16{}, f16{});
 }
 
 }  // namespace
@@ -381,7 +405,6 @@ __global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs a) {
 using namespace scd::feat;
 
 extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd_adamw_t* options, void* stream) {
-    constexpr int64_t kMost = int64_t(1) << 42;  // elements of a call: chunk numbers stay below 2^32
     if (count < 0 || (count > 0 && !spans)) return fail(SCD_ERR_INVALID, "bad spans");
     if (!options) return fail(SCD_ERR_INVALID, "options is null");
     const scd_adamw_t& o = *options;
@@ -390,7 +413,7 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
     if (!(std::isfinite(o.eps) && o.eps >= 0.0)) return fail(SCD_ERR_INVALID, "eps must be >= 0");
     if (o.norm_dev && !(o.max_norm >= 0.0f)) return fail(SCD_ERR_INVALID, "max_norm must be >= 0");
     if (!o.step_dev && o.step < 1) return fail(SCD_ERR_INVALID, "step must be >= 1");
-    int64_t total = 0;
+    int64_t total = 0, bytes = 0;
     for (int64_t i = 0; i < count; ++i) {
         const scd_adamw_span_t& t = spans[i];
         if (!type_bytes(t.param_type) || !type_bytes(t.grad_type) || (t.grad_type != t.param_type && t.grad_type != SCD_F32 && t.param_type != SCD_F32))
@@ -399,14 +422,13 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
         if (t.copy && (t.param_type != SCD_F32 || (t.copy_type != SCD_BF16 && t.copy_type != SCD_F16)))
             return fail(SCD_ERR_UNSUPPORTED, "span %lld: copies are bfloat16 or float16, of float32 parameters", (long long)i);
         if (!(std::isfinite(t.weight_decay) && t.weight_decay >= 0.0f)) return fail(SCD_ERR_INVALID, "span %lld: weight_decay must be >= 0", (long long)i);
-        if (t.n < 0 || t.n > kMost - total || (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (t.state_type == SCD_E4M3 && (!t.m_scale || !t.v_scale)))))
+        if (t.n < 0 || t.n > kStepMost - total || (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (t.state_type == SCD_E4M3 && (!t.m_scale || !t.v_scale)))))
             return fail(SCD_ERR_INVALID, "span %lld: bad size or null pointer", (long long)i);
         total += t.n;
+        bytes += t.n * (2 * type_bytes(t.param_type) + type_bytes(t.grad_type) + (t.state_type == SCD_F32 ? 16 : 4));
     }
     if (total == 0) return SCD_OK;
     StepArgs a;
-    // Small chunks where whole ones would leave CUs idle.
-    a.chunk = (uint32_t)(total < kStepChunk * kStepBlocks ? kStepChunk / 2 : kStepChunk);
     a.seed = o.seed;
     a.lr_dev = o.lr_dev;
     a.step_dev = o.step_dev;
@@ -424,18 +446,26 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
     a.rate = (float)(o.lr / -std::expm1((double)o.step * a.log_b1));
     a.root = (float)(1.0 / std::sqrt(-std::expm1((double)o.step * a.log_b2)));
     hipStream_t s = (hipStream_t)stream;
-    for (int64_t i = 0; i < count;) {
-        a.count = 0;
-        a.chunks = 0;
-        for (; i < count && a.count < kSteps; ++i) {
-            const scd_adamw_span_t& t = spans[i];
-            if (t.n == 0) continue;
-            a.first[a.count] = a.chunks;
-            a.s[a.count++] = Step{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, (uint32_t)i, t.weight_decay, (uint8_t)t.param_type,
-                                  (uint8_t)t.grad_type, (uint8_t)t.copy_type, (uint8_t)t.state_type, 0};
-            a.chunks += (uint32_t)ceil_div(t.n, (int64_t)a.chunk);
+    const bool once = bytes >= kStepOnce;
+    for (const bool eight : {false, true}) {
+        a.chunk = (uint32_t)(eight ? kStepChunk8 : kStepChunk);
+        for (int64_t i = 0; i < count;) {
+            a.count = 0;
+            a.chunks = 0;
+            for (; i < count && a.count < kSteps; ++i) {
+                const scd_adamw_span_t& t = spans[i];
+                if (t.n == 0 || (t.state_type == SCD_E4M3) != eight) continue;
+                a.first[a.count] = a.chunks;
+                a.s[a.count++] = Step{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, (uint32_t)i, t.weight_decay, (uint8_t)t.param_type,
+                                      (uint8_t)t.grad_type, (uint8_t)t.copy_type, (uint8_t)t.state_type, 0};
+                a.chunks += (uint32_t)ceil_div(t.n, (int64_t)a.chunk);
+            }
+            if (a.count == 0) continue;
+            if (eight)
+                once ? k_adamw<true, true><<<a.chunks, kStepThreads, 0, s>>>(a) : k_adamw<true, false><<<a.chunks, kStepThreads, 0, s>>>(a);
+            else
+                once ? k_adamw<false, true><<<a.chunks, kStepThreads, 0, s>>>(a) : k_adamw<false, false><<<a.chunks, kStepThreads, 0, s>>>(a);
         }
-        if (a.count) k_adamw<<<std::min<uint32_t>(kStepBlocks, a.chunks), kStepThreads, 0, s>>>(a);
     }
     return launched("scd_adamw");
 }
