@@ -23,14 +23,16 @@ namespace scd {
 namespace feat {
 namespace {
 
-constexpr int kStepThreads = 256;
-constexpr int kSteps = 44;          // tensors a launch: the arguments stay below 4 KB
-constexpr int kStateBlock = 256;    // elements that share a scale
-constexpr int64_t kStepChunk = 1024;   // elements of a workgroup, 32 bits
-constexpr int64_t kStepChunk8 = 2048;  // and 8
-// Elements of a call at most: a launch has fewer than 2^32 threads, though every tensor's last chunk may be short.
-constexpr int64_t kStepMost = (0xFFFFFF - kSteps) * kStepChunk;
-constexpr int64_t kStepOnce = int64_t(256) << 20;
+constexpr int kStepThreads = 64;
+constexpr int kSteps = 44;             // tensors a launch: the arguments stay below 4 KB
+constexpr int kStateBlock = 256;       // elements that share a scale
+constexpr int64_t kStepChunk = 256;    // elements of a workgroup, 32 bits
+constexpr int64_t kStepChunk8 = 512;   // and 8
+constexpr int64_t kStepBlocks = kMaxThreads / kStepThreads;  // workgroups of a launch at most
+constexpr int64_t kStepMost = int64_t(1) << 39;  // elements of a call: chunk numbers stay below 2^32
+constexpr int64_t kStepOnce = int64_t(448) << 20;
+// LDS that a workgroup of states in 32 bits asks for and does not use: sixteen to a CU.
+constexpr int kStepLds = 10240;
 
 struct Step {
     void* p;
@@ -52,6 +54,7 @@ struct StepArgs {
     uint32_t count;
     uint32_t chunks;
     uint32_t chunk;  // elements of a chunk
+    uint32_t from;   // the launch's first chunk
     uint32_t seed;
     const float* lr_dev;
     const int64_t* step_dev;
@@ -122,21 +125,25 @@ __device__ __forceinline__ void fetch_vec(const T* p, float (&o)[V]) {
     widen(fetch_raw<V, ONCE>(p), o);
 }
 
-// Eight values of 8 bits.
-typedef uint32_t Eight __attribute__((ext_vector_type(2), aligned(1)));
+template <bool ONCE, typename T>
+__device__ __forceinline__ void fetch_part(const T* p, float* o) {
+    const Raw<4, T> r = fetch_raw<4, ONCE>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = (float)r.t[k];
+}
+
+// Four values of 8 bits.
+typedef uint32_t Four __attribute__((aligned(1)));
 template <bool ONCE>
-__device__ __forceinline__ void fetch_8(uint32_t (&w)[2], const uint8_t* p) {
-    const Eight x = ONCE ? __builtin_nontemporal_load((const Eight*)p) : *(const Eight*)p;
-    w[0] = x[0];
-    w[1] = x[1];
+__device__ __forceinline__ uint32_t fetch_4(const uint8_t* p) {
+    return ONCE ? __builtin_nontemporal_load((const Four*)p) : *(const Four*)p;
 }
 template <bool ONCE>
-__device__ __forceinline__ void put_8(uint8_t* p, const uint32_t (&w)[2]) {
-    const Eight x = {w[0], w[1]};
+__device__ __forceinline__ void put_4(uint8_t* p, uint32_t w) {
     if (ONCE)
-        __builtin_nontemporal_store(x, (Eight*)p);
+        __builtin_nontemporal_store(w, (Four*)p);
     else
-        *(Eight*)p = x;
+        *(Four*)p = w;
 }
 
 // V elements from the i-th on, states in 32 bits.
@@ -252,34 +259,41 @@ __device__ __forceinline__ uint32_t random_r4(const float* x, const uint32_t* wo
     return out;
 }
 
-// Two blocks of a tensor, from the `at`-th element on, `n` elements of them: a wave.
+// Two blocks of a tensor, from the `at`-th element on, `n` elements of them: a wave.  Half of it takes a block, each lane four
+// elements of its first half and four of its second, so that every access of the wave is to whole lines.
 template <bool ONCE, typename P, typename G>
 __device__ __forceinline__ void blocks_8(const Common& c, const Step& s, float keep, int64_t at, int32_t n) {
-    constexpr int V = 8;
-    const int32_t lane = threadIdx.x % 64, i = lane * V;
-    const int64_t from = at + i, block = from / kStateBlock;
-    const bool whole = i + V <= n, there = i / kStateBlock * kStateBlock < n;
-    float p[V] = {}, g[V] = {};
+    constexpr int V = 8, kApart = kStateBlock / 2;
+    const int32_t lane = threadIdx.x % 64, begin = lane / 32 * kStateBlock, i = begin + lane % 32 * 4;
+    const int64_t from = at + i, block = (at + begin) / kStateBlock;
+    const bool there = begin < n, whole = i + kApart + 4 <= n;
+    float p[V] = {}, g[V] = {}, m[V], r[V];
     uint32_t mw[2] = {}, rw[2] = {};
     uint8_t* const mq = (uint8_t*)s.m + from;
     uint8_t* const rq = (uint8_t*)s.v + from;
+    P* const pp = (P*)s.p + from;
+    const G* const pg = (const G*)s.g + from;
     if (whole) {
-        fetch_vec<ONCE>((const P*)s.p + from, p);
-        fetch_vec<ONCE>((const G*)s.g + from, g);
-        fetch_8<ONCE>(mw, mq);
-        fetch_8<ONCE>(rw, rq);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            fetch_part<ONCE>(pp + j * kApart, p + 4 * j);
+            fetch_part<ONCE>(pg + j * kApart, g + 4 * j);
+            mw[j] = fetch_4<ONCE>(mq + j * kApart);
+            rw[j] = fetch_4<ONCE>(rq + j * kApart);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (i + k < n) {
-                p[k] = (float)((const P*)s.p)[from + k];
-                g[k] = (float)((const G*)s.g)[from + k];
-                mw[k / 4] |= (uint32_t)mq[k] << (8 * (k % 4));
-                rw[k / 4] |= (uint32_t)rq[k] << (8 * (k % 4));
+        for (int k = 0; k < V; ++k) {
+            const int32_t e = k / 4 * kApart + k % 4;
+            if (i + e < n) {
+                p[k] = (float)pp[e];
+                g[k] = (float)pg[e];
+                mw[k / 4] |= (uint32_t)mq[e] << (8 * (k % 4));
+                rw[k / 4] |= (uint32_t)rq[e] << (8 * (k % 4));
             }
+        }
     }
     const float ms = there ? s.ms[block] : 0.0f, rs = there ? s.vs[block] : 0.0f;
-    float m[V], r[V];
 #pragma unroll
     for (int k = 0; k < V / 4; ++k) {
         const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mw[k], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mw[k], true);
@@ -303,16 +317,22 @@ __device__ __forceinline__ void blocks_8(const Common& c, const Step& s, float k
 #pragma unroll
     for (int k = 0; k < V; ++k) p[k] = p[k] * keep - c.rate * m[k] * __builtin_amdgcn_rcpf(r[k] * c.root + c.eps);
     if (whole) {
-        put_vec<ONCE>((P*)s.p + from, p);
-        if (s.copy) store_copy<ONCE>(s.copy, s.ct, from, p);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float four[4] = {p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]};
+            put_vec<ONCE>(pp + j * kApart, four);
+            if (s.copy) store_copy<ONCE>(s.copy, s.ct, from + j * kApart, four);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (i + k < n) {
+        for (int k = 0; k < V; ++k) {
+            const int32_t e = k / 4 * kApart + k % 4;
+            if (i + e < n) {
                 const float one[1] = {p[k]};
-                store_vec((P*)s.p + from + k, one);
-                if (s.copy) store_copy<false>(s.copy, s.ct, from + k, one);
+                store_vec(pp + e, one);
+                if (s.copy) store_copy<false>(s.copy, s.ct, from + e, one);
             }
+        }
     }
     uint32_t most_m = 0, most_r = 0;
 #pragma unroll
@@ -344,27 +364,32 @@ __device__ __forceinline__ void blocks_8(const Common& c, const Step& s, float k
 #pragma unroll
         for (int l = 0; l < 4; ++l) {
             float& x = r[4 * k + l];
-            word[l] = murmur_fmix32((uint32_t)(from + 4 * k + l) ^ key);
+            word[l] = murmur_fmix32((uint32_t)(from + k * kApart + l) ^ key);
             m[4 * k + l] = scaled(m[4 * k + l], to_m, im);
             x = x == 0.0f ? 0.0f : fmaxf(scaled(x, to_r, ir), kLeast);
         }
         mw[k] = random_m4(m + 4 * k, word);
         rw[k] = random_r4(r + 4 * k, word) | lost[k];
     }
-    if (there && i % kStateBlock == 0) {
+    if (there && i == begin) {
         s.ms[block] = to_m;
         s.vs[block] = to_r;
     }
     if (whole) {
-        put_8<ONCE>(mq, mw);
-        put_8<ONCE>(rq, rw);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            put_4<ONCE>(mq + j * kApart, mw[j]);
+            put_4<ONCE>(rq + j * kApart, rw[j]);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (i + k < n) {
-                mq[k] = (uint8_t)(mw[k / 4] >> (8 * (k % 4)));
-                rq[k] = (uint8_t)(rw[k / 4] >> (8 * (k % 4)));
+        for (int k = 0; k < V; ++k) {
+            const int32_t e = k / 4 * kApart + k % 4;
+            if (i + e < n) {
+                mq[e] = (uint8_t)(mw[k / 4] >> (8 * (k % 4)));
+                rq[e] = (uint8_t)(rw[k / 4] >> (8 * (k % 4)));
             }
+        }
     }
 }
 
@@ -380,7 +405,7 @@ __device__ __forceinline__ void chunk_8(const Common& c, const Step& s, int64_t 
 template <bool EIGHT, bool ONCE>
 __global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs a) {
     const Common c = common_of(a);
-    const uint32_t chunk = blockIdx.x, k = tensor_of(a, chunk);
+    const uint32_t chunk = a.from + blockIdx.x, k = tensor_of(a, chunk);
     const Step& s = a.s[k];
     const int64_t at = (int64_t)(chunk - a.first[k]) * a.chunk;
     const int32_t n = (int32_t)min((int64_t)a.chunk, s.n - at);
@@ -425,7 +450,7 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
         if (t.n < 0 || t.n > kStepMost - total || (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (t.state_type == SCD_E4M3 && (!t.m_scale || !t.v_scale)))))
             return fail(SCD_ERR_INVALID, "span %lld: bad size or null pointer", (long long)i);
         total += t.n;
-        bytes += t.n * (2 * type_bytes(t.param_type) + type_bytes(t.grad_type) + (t.state_type == SCD_F32 ? 16 : 4));
+        bytes += t.n * (2 * type_bytes(t.param_type) + type_bytes(t.grad_type) + (t.state_type == SCD_F32 ? 16 : 4) + (t.copy ? 2 : 0));
     }
     if (total == 0) return SCD_OK;
     StepArgs a;
@@ -460,11 +485,14 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
                                       (uint8_t)t.grad_type, (uint8_t)t.copy_type, (uint8_t)t.state_type, 0};
                 a.chunks += (uint32_t)ceil_div(t.n, (int64_t)a.chunk);
             }
-            if (a.count == 0) continue;
-            if (eight)
-                once ? k_adamw<true, true><<<a.chunks, kStepThreads, 0, s>>>(a) : k_adamw<true, false><<<a.chunks, kStepThreads, 0, s>>>(a);
-            else
-                once ? k_adamw<false, true><<<a.chunks, kStepThreads, 0, s>>>(a) : k_adamw<false, false><<<a.chunks, kStepThreads, 0, s>>>(a);
+            for (int64_t from = 0; from < a.chunks; from += kStepBlocks) {
+                a.from = (uint32_t)from;
+                const uint32_t blocks = (uint32_t)std::min<int64_t>(kStepBlocks, a.chunks - from);
+                if (eight)
+                    once ? k_adamw<true, true><<<blocks, kStepThreads, 0, s>>>(a) : k_adamw<true, false><<<blocks, kStepThreads, 0, s>>>(a);
+                else
+                    once ? k_adamw<false, true><<<blocks, kStepThreads, kStepLds, s>>>(a) : k_adamw<false, false><<<blocks, kStepThreads, kStepLds, s>>>(a);
+            }
         }
     }
     return launched("scd_adamw");
