@@ -91,10 +91,10 @@ __global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
     const auto fetch = [&](int64_t row) {
         row = min(row, (int64_t)a.rows - 1);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) next[j] = load_raw<VEC>(a.x + row * a.xstride + col.at[j]);
+        for (int j = 0; j < NV; ++j) next[j] = fetch_raw<VEC, ONCE>(a.x + row * a.xstride + col.at[j]);
         if (a.res)
 #pragma unroll
-            for (int j = 0; j < NV; ++j) more[j] = load_raw<VEC>(a.res + row * a.rstride + col.at[j]);
+            for (int j = 0; j < NV; ++j) more[j] = fetch_raw<VEC, ONCE>(a.res + row * a.rstride + col.at[j]);
     };
     fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
     if (a.weight)
@@ -336,7 +336,9 @@ __global__ void __launch_bounds__(THREADS) k_rms_grad(RmsGradArgs<T, P> a) {
             for (int j = 0; j < NV; ++j) nres[j] = fetch_raw<VEC, ONCE>(a.res + row * a.rstride + col.at[j]);
         nrstd = a.rstd[row];
     };
-    fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
+    // The next row is loaded before this one is worked on, but not where the threads' registers do not hold both.
+    constexpr bool kAhead = THREADS <= 512;
+    if (kAhead) fetch((int64_t)blockIdx.x * kGroups + threadIdx.x / LPR);
     const auto weights = [&](int j) {
         if (a.weight)
             w[j] = load_raw<VEC>(a.weight + col.at[j]);
@@ -351,6 +353,7 @@ __global__ void __launch_bounds__(THREADS) k_rms_grad(RmsGradArgs<T, P> a) {
     for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
         const int64_t r = r0 + threadIdx.x / LPR;
         const bool here = r < a.rows;
+        if (!kAhead) fetch(r);
         const float rstd = nrstd;
         float g[NV][VEC], n[NV][VEC], res[NV][VEC], s[1] = {0.0f};
 #pragma unroll
@@ -363,7 +366,7 @@ __global__ void __launch_bounds__(THREADS) k_rms_grad(RmsGradArgs<T, P> a) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) res[j][i] = 0.0f;
         }
-        if (r0 + step < a.rows) fetch(r + step);
+        if (kAhead && r0 + step < a.rows) fetch(r + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float wj[VEC];
@@ -485,22 +488,23 @@ __global__ void __launch_bounds__(kWideThreads) k_rms_grad_wide(RmsGradArgs<T, P
     }
 }
 
-// dw: the workgroups' sums, 64 columns a workgroup, in kSlices interleaved parts that are added in order.
+// dw: the workgroups' sums, kAcross columns a workgroup, in kSlices interleaved parts that are added in order.
+constexpr int kAcross = 32;
 constexpr int kSlices = 16;
 
 template <typename P>
-__global__ void __launch_bounds__(64 * kSlices) k_rms_params(const float* __restrict__ sums, int32_t parts, int32_t dim, P* __restrict__ dw) {
-    __shared__ float lds[kSlices][64];
-    const int32_t c = blockIdx.x * 64 + threadIdx.x % 64, slice = threadIdx.x / 64;
+__global__ void __launch_bounds__(kAcross * kSlices) k_rms_params(const float* __restrict__ sums, int32_t parts, int32_t dim, P* __restrict__ dw) {
+    __shared__ float lds[kSlices][kAcross];
+    const int32_t column = threadIdx.x % kAcross, c = blockIdx.x * kAcross + column, slice = threadIdx.x / kAcross;
     float s = 0.0f;
     if (c < dim)
 #pragma unroll 8
         for (int32_t p = slice; p < parts; p += kSlices) s += sums[(int64_t)p * dim + c];
-    lds[slice][threadIdx.x % 64] = s;
+    lds[slice][column] = s;
     __syncthreads();
     if (slice == 0 && c < dim) {
 #pragma unroll
-        for (int k = 1; k < kSlices; ++k) s += lds[k][threadIdx.x];
+        for (int k = 1; k < kSlices; ++k) s += lds[k][column];
         dw[c] = (P)s;
     }
 }
@@ -508,12 +512,33 @@ __global__ void __launch_bounds__(64 * kSlices) k_rms_params(const float* __rest
 // ---------------------------------------------------------------------------------------- host
 
 constexpr int kRmsThreads = 256;      // a workgroup, where a row's group is not wider
-constexpr int kRmsBlocks = 2048;      // workgroups at most: eight to each CU
-constexpr int kRmsGradBlocks = 512;   // the backward pass's, whose sums of dw go through memory
+constexpr int64_t kRmsBlocks = 65536;
+constexpr int64_t kRmsBlocksNarrow = 8192;
+constexpr int64_t kRmsBlocksWide = 2048;
+constexpr int kRmsGradBlocks = 256;   // the backward pass's, whose sums of dw go through memory
 constexpr int kRmsGradBlocksWide = 256;
 constexpr int64_t kRmsTurnsAlone = 4;  // rows for each group of a workgroup up to which one workgroup does it all
-constexpr int64_t kRmsOnceOut = int64_t(64) << 20;
-constexpr int64_t kRmsOnceBytes = int64_t(288) << 20;
+constexpr int64_t kRmsOnce = int64_t(384) << 20;      // bytes of all matrices
+constexpr int64_t kRmsOnce8 = int64_t(288) << 20;
+constexpr int64_t kRmsGradOnce = int64_t(320) << 20;
+constexpr int kRmsGradThreads = 512;
+
+// with_group for the backward pass, whose widest rows take 1,024 threads.
+template <typename T, typename F>
+bool with_grad_group(int64_t dim, F&& f) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t vecs = ceil_div(dim, V);
+    if (vecs <= 1024) return with_group<T, true>(dim, f);
+    if (vecs <= 2048)
+        f(Int<V>{}, Int<2>{}, Int<1024>{});
+    else if constexpr (V == 4) {
+        if (vecs > 4096) return false;
+        f(Int<V>{}, Int<4>{}, Int<1024>{});
+    } else {
+        return false;
+    }
+    return true;
+}
 
 int check_rms(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {
     if (!type_bytes(type) || (param_type != type && param_type != SCD_F32))
@@ -554,17 +579,18 @@ extern "C" int scd_rms_norm(const void* x, int32_t type, int64_t x_stride, const
         using P = decltype(p);
         const RmsArgs<T, P> a{(const T*)x, x_stride, (const T*)residual, residual_stride, (int32_t)rows, (int32_t)dim, (const P*)weight, eps,
                               (int32_t)group, (int32_t)(group ? ceil_div(dim, group) : 1), y, y_stride, scale, residual ? (T*)sum : nullptr, sum_stride, rstd};
-        const bool once = rows * dim * (int64_t)sizeof(T) >= kRmsOnceOut;
+        const int64_t matrices = rows * dim * (int64_t)sizeof(T) * (residual ? 3 : 1);
+        const bool once = eight ? matrices + rows * dim > kRmsOnce8 : matrices + rows * dim * (int64_t)sizeof(T) > kRmsOnce;
         const bool fits = with_group<T, false>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kRmsThreads ? LPR : kRmsThreads;
-            const uint32_t blocks = (uint32_t)std::min<int64_t>(kRmsBlocks, ceil_div(rows, THREADS / LPR));
+            const uint32_t blocks = (uint32_t)std::min<int64_t>(LPR <= 64 ? kRmsBlocksNarrow : LPR <= 256 ? kRmsBlocks : kRmsBlocksWide, ceil_div(rows, THREADS / LPR));
             if (eight)
                 once ? k_rms<VEC, NV, LPR, THREADS, true, true><<<blocks, THREADS, 0, s>>>(a) : k_rms<VEC, NV, LPR, THREADS, true, false><<<blocks, THREADS, 0, s>>>(a);
             else
                 once ? k_rms<VEC, NV, LPR, THREADS, false, true><<<blocks, THREADS, 0, s>>>(a) : k_rms<VEC, NV, LPR, THREADS, false, false><<<blocks, THREADS, 0, s>>>(a);
         });
-        const uint32_t blocks = (uint32_t)std::min<int64_t>(kRmsBlocks, rows);
+        const uint32_t blocks = (uint32_t)std::min<int64_t>(kRmsBlocksWide, rows);
         if (!fits) eight ? k_rms_wide<true><<<blocks, kWideThreads, 0, s>>>(a) : k_rms_wide<false><<<blocks, kWideThreads, 0, s>>>(a);
     });
     return launched("scd_rms_norm");
@@ -600,15 +626,15 @@ extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const vo
         RmsGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)h, h_stride, (const T*)residual_grad, residual_stride, rstd, (int32_t)rows,
                             (int32_t)dim, (const P*)weight, (T*)dh, dh_stride, nullptr, nullptr};
         int64_t blocks = 0;  // whose sums go through the workspace
-        const bool fits = rows > 0 && with_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
+        const bool fits = rows > 0 && with_grad_group<T>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
-            constexpr int THREADS = LPR > kRmsThreads ? LPR : kRmsThreads;
+            constexpr int THREADS = LPR > kRmsGradThreads ? LPR : kRmsGradThreads;
             constexpr int64_t groups = THREADS / LPR;
             const bool alone = rows <= (LPR >= 512 ? 1 : kRmsTurnsAlone) * groups;
             blocks = alone && dweight ? 1 : std::min<int64_t>(LPR >= 512 ? kRmsGradBlocksWide : kRmsGradBlocks, ceil_div(rows, groups));
             a.dw = alone ? (P*)dweight : nullptr;
             a.sums = alone || !dweight ? nullptr : (float*)workspace;
-            if (rows * dim * 3 * (int64_t)sizeof(T) < kRmsOnceBytes)
+            if (rows * dim * (residual_grad ? 4 : 3) * (int64_t)sizeof(T) <= kRmsGradOnce)
                 k_rms_grad<VEC, NV, LPR, THREADS, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
             else
                 k_rms_grad<VEC, NV, LPR, THREADS, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
@@ -621,10 +647,10 @@ extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const vo
                 a.sums = (float*)workspace;
                 k_rms_columns<<<dim3((uint32_t)across, (uint32_t)blocks), kColumnThreads, 0, s>>>(a);
             }
-            k_rms_grad_wide<<<(uint32_t)std::min<int64_t>(kRmsBlocks, rows), kWideThreads, 0, s>>>(a);
+            k_rms_grad_wide<<<(uint32_t)std::min<int64_t>(kRmsBlocksWide, rows), kWideThreads, 0, s>>>(a);
         }
         if (dweight && !a.dw)  // without rows: zeros
-            k_rms_params<<<(uint32_t)ceil_div(dim, 64), 64 * kSlices, 0, s>>>((const float*)workspace, (int32_t)blocks, (int32_t)dim, (P*)dweight);
+            k_rms_params<<<(uint32_t)ceil_div(dim, kAcross), kAcross * kSlices, 0, s>>>((const float*)workspace, (int32_t)blocks, (int32_t)dim, (P*)dweight);
     });
     return launched("scd_rms_norm_grad");
 }
