@@ -92,7 +92,8 @@ def _binding_lacks() -> list:
     spec = importlib.util.find_spec("torch")
     headers = {"Python.h": sysconfig.get_paths()["include"]}
     if spec and spec.origin:
-        headers["torch/csrc/autograd/python_variable.h"] = os.path.join(os.path.dirname(spec.origin), "include")
+        for header in ("torch/csrc/autograd/python_variable.h", "ATen/hip/EmptyTensor.h"):
+            headers[header] = os.path.join(os.path.dirname(spec.origin), "include")
     lacks = [h for h, where in headers.items() if not os.path.exists(os.path.join(where, h))]
     return lacks + [what for what, there in (("torch", spec), ("g++", shutil.which("g++"))) if not there]
 
@@ -106,7 +107,7 @@ def _compile_binding(verbose):
     _finish(_run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-Wno-unused-parameter",
                   f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
                   *(f for p in includes for f in ("-isystem", p)), BINDING_SOURCE, "-o", tmp,
-                  *(f for p in cpp_extension.library_paths() for f in ("-L", p)), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
+                  *(f for p in cpp_extension.library_paths() for f in ("-L", p)), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10",
                   "-L", HERE, "-l:libscd.so", "-Wl,-rpath,$ORIGIN"], verbose), verbose)
     os.replace(tmp, BINDING)
 

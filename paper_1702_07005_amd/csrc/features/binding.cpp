@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/Allocator.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/Dtype.h>
@@ -127,8 +128,9 @@ int32_t token_type(const at::Tensor& tokens, const at::Device& device) {
     return s == at::kInt ? SCD_I32 : SCD_I64;
 }
 
+// What at::empty makes, without its way through the dispatcher.
 at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Device& device) {
-    return at::empty(sizes, at::TensorOptions().dtype(type).device(device));
+    return at::detail::empty_cuda(sizes, type, device, std::nullopt);
 }
 
 // The calls are outside autograd: they record nothing.  A caller's tensor that they write to counts the write, as

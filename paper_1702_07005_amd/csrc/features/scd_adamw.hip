@@ -30,7 +30,7 @@ constexpr int64_t kStepChunk = 256;    // elements of a workgroup, 32 bits
 constexpr int64_t kStepChunk8 = 512;   // and 8
 constexpr int64_t kStepBlocks = kMaxThreads / kStepThreads;  // workgroups of a launch at most
 constexpr int64_t kStepMost = int64_t(1) << 39;  // elements of a call: chunk numbers stay below 2^32
-constexpr int64_t kStepOnce = int64_t(448) << 20;
+constexpr int64_t kStepOnce = int64_t(128) << 20;
 // LDS that a workgroup of states in 32 bits asks for and does not use: sixteen to a CU.
 constexpr int kStepLds = 10240;
 

@@ -177,33 +177,39 @@ __global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
     }
 }
 
-// n of a vector's elements, the rest zeros.
-template <int V, typename T>
-__device__ __forceinline__ void load_some(const T* p, int32_t n, float (&o)[V]) {
-    if (n >= V) {
-        load_vec(p, o);
-    } else {
+// Rows too wide for the registers are read again from the caches: a workgroup takes a row, and each thread its vectors of V
+// elements, kAtOnce of them loaded before the first is used.  As in vec_column, the last vector begins early, and its
+// first `skip` columns, which another thread has, are neither counted nor written: where the output takes an input's
+// place they may hold either.  Each thread reads again what it wrote itself.
+constexpr int kAtOnce = 4;
+
+// The columns of a thread's next vectors; from the row's end on, the last one with all its columns skipped.
+template <int V, int APART>
+struct Vectors {
+    int32_t at[kAtOnce], skip[kAtOnce];
+    __device__ __forceinline__ Vectors(int32_t c, int32_t dim) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = i < n ? (float)p[i] : 0.0f;
+        for (int u = 0; u < kAtOnce; ++u) {
+            at[u] = min(c + u * APART, dim - V);
+            skip[u] = min(c + u * APART - at[u], V);
+        }
     }
-}
+};
 
 template <int V, typename T>
-__device__ __forceinline__ void store_some(T* p, int32_t n, const float (&v)[V]) {
-    if (n >= V) {
+__device__ __forceinline__ void store_from(T* p, int32_t skip, const float (&v)[V]) {
+    if (skip == 0) {
         store_vec(p, v);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i < n) p[i] = (T)v[i];
+            if (i >= skip) p[i] = (T)v[i];
     }
 }
 
-// Rows too wide for the registers: a workgroup reads its row again from the caches, twice, or three times where 8 bits with
-// one scale for the row need the largest value first.  Each thread reads again what it wrote itself.
 template <bool Q, typename T, typename P>
 __global__ void __launch_bounds__(kWideThreads) k_rms_wide(RmsArgs<T, P> a) {
-    constexpr int V = 16 / sizeof(T), kStep = kWideThreads * V;
+    constexpr int V = 16 / sizeof(T), kApart = kWideThreads * V, kStep = kAtOnce * kApart;
     __shared__ float lds[lds_words<kWideThreads, kWideThreads>(1)];
     const float inv = 1.0f / (float)a.dim;
     int turn = 0;
@@ -214,33 +220,51 @@ __global__ void __launch_bounds__(kWideThreads) k_rms_wide(RmsArgs<T, P> a) {
         const T* const kept = res ? sum : x;
         float s[1] = {0.0f};
         for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
-            const int32_t n = min(V, a.dim - c);
-            float h[V];
-            load_some(x + c, n, h);
-            if (res) {
-                float more[V];
-                load_some(res + c, n, more);
+            const Vectors<V, kApart> col(c, a.dim);
+            Raw<V, T> rx[kAtOnce], rr[kAtOnce];
 #pragma unroll
-                for (int i = 0; i < V; ++i) h[i] = (float)(T)(h[i] + more[i]);
-                store_some(sum + c, n, h);
+            for (int u = 0; u < kAtOnce; ++u) rx[u] = load_raw<V>(x + col.at[u]);
+            if (res)
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) rr[u] = load_raw<V>(res + col.at[u]);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                float h[V];
+                widen(rx[u], h);
+                if (res) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[i] = (float)(T)(h[i] + (float)rr[u].t[i]);
+                    store_from(sum + col.at[u], col.skip[u], h);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[0] += i >= col.skip[u] ? h[i] * h[i] : 0.0f;
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += h[i] * h[i];
         }
         group_sums<kWideThreads, kWideThreads, 1>(s, lds, turn);
         turn ^= 1;
         const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
-        const auto result = [&](int32_t c, int32_t n, float(&y)[V]) {
-            float w[V];
-            load_some(kept + c, n, y);
-            if (a.weight) load_some(a.weight + c, n, w);
+        // f(u, the results of the thread's u-th vector), all vectors of a step
+        const auto results = [&](const Vectors<V, kApart>& col, auto&& f) {
+            Raw<V, T> rx[kAtOnce];
+            Raw<V, P> rw[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = y[i] * rstd * (a.weight ? w[i] : 1.0f);
+            for (int u = 0; u < kAtOnce; ++u) rx[u] = load_raw<V>(kept + col.at[u]);
+            if (a.weight)
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) rw[u] = load_raw<V>(a.weight + col.at[u]);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                float y[V];
+                widen(rx[u], y);
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = y[i] * rstd * (a.weight ? (float)rw[u].t[i] : 1.0f);
+                f(u, y);
+            }
         };
-        const auto largest = [&](const float(&y)[V]) {
+        const auto largest = [&](const float(&y)[V], int32_t skip) {
             float most = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) most = fmaxf(most, fabsf(y[i]));
+            for (int i = 0; i < V; ++i) most = fmaxf(most, i >= skip ? fabsf(y[i]) : 0.0f);
             return most;
         };
         if constexpr (Q) {
@@ -248,9 +272,8 @@ __global__ void __launch_bounds__(kWideThreads) k_rms_wide(RmsArgs<T, P> a) {
             if (a.group == 0) {
                 float most = 0.0f;
                 for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
-                    float y[V];
-                    result(c, min(V, a.dim - c), y);
-                    most = fmaxf(most, largest(y));
+                    const Vectors<V, kApart> col(c, a.dim);
+                    results(col, [&](int u, const float(&y)[V]) { most = fmaxf(most, largest(y, col.skip[u])); });
                 }
                 scale = e4m3_scale(row_max<kWideThreads, kWideThreads>(most, lds, turn));
                 turn ^= 1;
@@ -258,31 +281,25 @@ __global__ void __launch_bounds__(kWideThreads) k_rms_wide(RmsArgs<T, P> a) {
             }
             uint8_t* const q = (uint8_t*)a.y + r * a.ystride;
             for (int32_t c0 = 0; c0 < a.dim; c0 += kStep) {  // all lanes of a wave go on to its groups' last one
-                const int32_t c = c0 + threadIdx.x * V, n = min(V, a.dim - c);
-                float y[V] = {};
-                if (n > 0) result(c, n, y);
-                if (a.group) {
-                    scale = e4m3_scale(group_max<32>(largest(y), a.group / V));
-                    if (n > 0 && c % a.group == 0) a.scale[r * a.scales + c / a.group] = scale;
-                }
-                const float to = 1.0f / scale;
+                const int32_t c = c0 + threadIdx.x * V;
+                const Vectors<V, kApart> col(c, a.dim);
+                results(col, [&](int u, float(&y)[V]) {
+                    if (a.group) {
+                        scale = e4m3_scale(group_max<32>(largest(y, col.skip[u]), a.group / V));
+                        const int32_t first = c + u * kApart;
+                        if (first < a.dim && first % a.group == 0) a.scale[r * a.scales + first / a.group] = scale;
+                    }
+                    const float to = 1.0f / scale;
 #pragma unroll
-                for (int i = 0; i < V; ++i) y[i] *= to;
-                if (n == V) {
-                    store_e4m3<V>(q + c, y, 0);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (i < n) q[c + i] = (uint8_t)e4m3_pack4(y[i], 0.0f, 0.0f, 0.0f);
-                }
+                    for (int i = 0; i < V; ++i) y[i] *= to;
+                    if (col.skip[u] < V) store_e4m3<V>(q + col.at[u], y, col.skip[u]);
+                });
             }
         } else {
-            T* const y = (T*)a.y + r * a.ystride;
+            T* const out = (T*)a.y + r * a.ystride;
             for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
-                const int32_t n = min(V, a.dim - c);
-                float o[V];
-                result(c, n, o);
-                store_some(y + c, n, o);
+                const Vectors<V, kApart> col(c, a.dim);
+                results(col, [&](int u, const float(&y)[V]) { store_from(out + col.at[u], col.skip[u], y); });
             }
         }
         if (threadIdx.x == 0 && a.rstd) a.rstd[r] = rstd;
@@ -423,67 +440,93 @@ __global__ void __launch_bounds__(THREADS) k_rms_grad(RmsGradArgs<T, P> a) {
     }
 }
 
-// Wide rows: dw by columns, which the row kernel after it may overwrite the inputs of.  A thread takes a vector of columns
-// and every gridDim.y-th row.
+// Wide rows: dw by columns, before the row kernel, which may overwrite the inputs.  A thread takes a vector of columns and
+// every gridDim.y-th row.
 constexpr int kColumnThreads = 256;
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(kColumnThreads) k_rms_columns(RmsGradArgs<T, P> a) {
     constexpr int V = 16 / sizeof(T);
-    const int32_t c = (blockIdx.x * kColumnThreads + threadIdx.x) * V, n = min(V, a.dim - c);
-    if (n <= 0) return;
+    const int32_t k = blockIdx.x * kColumnThreads + threadIdx.x;
+    int32_t skip;
+    const int32_t c = vec_column<V>(k, a.dim, skip);
+    if (skip >= V) return;
     float dw[V] = {};
-#pragma unroll 4
-    for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
-        const float rstd = a.rstd[r];
-        float g[V], h[V];
-        load_some(a.dy + r * a.gstride + c, n, g);
-        load_some(a.h + r * a.hstride + c, n, h);
+    for (int64_t r0 = blockIdx.y; r0 < a.rows; r0 += (int64_t)gridDim.y * kAtOnce) {
+        Raw<V, T> rg[kAtOnce], rh[kAtOnce];
+        float rstd[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < V; ++i) dw[i] += g[i] * (h[i] * rstd);
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t r = min(r0 + (int64_t)u * gridDim.y, (int64_t)a.rows - 1);
+            rg[u] = load_raw<V>(a.dy + r * a.gstride + c);
+            rh[u] = load_raw<V>(a.h + r * a.hstride + c);
+            rstd[u] = a.rstd[r];
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (r0 + (int64_t)u * gridDim.y < a.rows)
+#pragma unroll
+                for (int i = 0; i < V; ++i) dw[i] += (float)rg[u].t[i] * ((float)rh[u].t[i] * rstd[u]);
     }
     if (a.dw)
-        store_some(a.dw + c, n, dw);
+        store_from(a.dw + c, skip, dw);
     else
-        store_some(a.sums + (int64_t)blockIdx.y * a.dim + c, n, dw);
+        store_from(a.sums + (int64_t)blockIdx.y * a.dim + c, skip, dw);
 }
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(kWideThreads) k_rms_grad_wide(RmsGradArgs<T, P> a) {
-    constexpr int V = 16 / sizeof(T), kStep = kWideThreads * V;
+    constexpr int V = 16 / sizeof(T), kApart = kWideThreads * V, kStep = kAtOnce * kApart;
     __shared__ float lds[lds_words<kWideThreads, kWideThreads>(1)];
     const float inv = 1.0f / (float)a.dim;
     int turn = 0;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
         const float rstd = a.rstd[r];
-        const auto load = [&](int32_t c, int32_t k, float(&g)[V], float(&n)[V]) {
-            load_some(a.dy + r * a.gstride + c, k, g);
-            load_some(a.h + r * a.hstride + c, k, n);
-            float w[V];
-            if (a.weight) load_some(a.weight + c, k, w);
+        const T* const dy = a.dy + r * a.gstride;
+        const T* const h = a.h + r * a.hstride;
+        const T* const more = a.res ? a.res + r * a.rstride : nullptr;
+        T* const dh = a.dh + r * a.dstride;
+        // f(u, g, n) for the thread's vectors of a step
+        const auto values = [&](const Vectors<V, kApart>& col, auto&& f) {
+            Raw<V, T> rg[kAtOnce], rh[kAtOnce];
+            Raw<V, P> rw[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                n[i] *= rstd;
-                g[i] *= a.weight ? w[i] : 1.0f;
+            for (int u = 0; u < kAtOnce; ++u) rg[u] = load_raw<V>(dy + col.at[u]);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) rh[u] = load_raw<V>(h + col.at[u]);
+            if (a.weight)
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) rw[u] = load_raw<V>(a.weight + col.at[u]);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                float g[V], n[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    n[i] = (float)rh[u].t[i] * rstd;
+                    g[i] = (float)rg[u].t[i] * (a.weight ? (float)rw[u].t[i] : 1.0f);
+                }
+                f(u, g, n);
             }
         };
         float s[1] = {0.0f};
         for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
-            float g[V], n[V];
-            load(c, min(V, a.dim - c), g, n);
+            const Vectors<V, kApart> col(c, a.dim);
+            values(col, [&](int u, const float(&g)[V], const float(&n)[V]) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += g[i] * n[i];
+                for (int i = 0; i < V; ++i) s[0] += i >= col.skip[u] ? g[i] * n[i] : 0.0f;
+            });
         }
         group_sums<kWideThreads, kWideThreads, 1>(s, lds, turn);
         const float mean = s[0] * inv;
         for (int32_t c = threadIdx.x * V; c < a.dim; c += kStep) {
-            const int32_t k = min(V, a.dim - c);
-            float g[V], n[V], res[V] = {};
-            load(c, k, g, n);
-            if (a.res) load_some(a.res + r * a.rstride + c, k, res);
+            const Vectors<V, kApart> col(c, a.dim);
+            values(col, [&](int u, float(&g)[V], const float(&n)[V]) {
+                float res[V] = {};
+                if (more) load_vec(more + col.at[u], res);
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = rstd * (g[i] - n[i] * mean) + res[i];
-            store_some(a.dh + r * a.dstride + c, k, g);
+                for (int i = 0; i < V; ++i) g[i] = rstd * (g[i] - n[i] * mean) + res[i];
+                if (col.skip[u] < V) store_from(dh + col.at[u], col.skip[u], g);
+            });
         }
     }
 }
@@ -513,15 +556,20 @@ __global__ void __launch_bounds__(kAcross * kSlices) k_rms_params(const float* _
 
 constexpr int kRmsThreads = 256;      // a workgroup, where a row's group is not wider
 constexpr int64_t kRmsBlocks = 65536;
-constexpr int64_t kRmsBlocksNarrow = 8192;
+constexpr int64_t kRmsBlocksNarrow = 16384;
+constexpr int64_t kRmsBlocks8 = 8192;
 constexpr int64_t kRmsBlocksWide = 2048;
 constexpr int kRmsGradBlocks = 256;   // the backward pass's, whose sums of dw go through memory
 constexpr int kRmsGradBlocksWide = 256;
+constexpr int64_t kColumnBlocks = 1024;  // of the sums by columns, which are at least nine across: fewer than 256 a column
 constexpr int64_t kRmsTurnsAlone = 4;  // rows for each group of a workgroup up to which one workgroup does it all
 constexpr int64_t kRmsOnce = int64_t(384) << 20;      // bytes of all matrices
 constexpr int64_t kRmsOnce8 = int64_t(288) << 20;
 constexpr int64_t kRmsGradOnce = int64_t(320) << 20;
 constexpr int kRmsGradThreads = 512;
+
+// Workgroups for `turns` turns, `most` of them at most, each with as many turns.
+int64_t even_blocks(int64_t turns, int64_t most) { return ceil_div(turns, ceil_div(turns, most)); }
 
 // with_group for the backward pass, whose widest rows take 1,024 threads.
 template <typename T, typename F>
@@ -584,7 +632,7 @@ extern "C" int scd_rms_norm(const void* x, int32_t type, int64_t x_stride, const
         const bool fits = with_group<T, false>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kRmsThreads ? LPR : kRmsThreads;
-            const uint32_t blocks = (uint32_t)std::min<int64_t>(LPR <= 64 ? kRmsBlocksNarrow : LPR <= 256 ? kRmsBlocks : kRmsBlocksWide, ceil_div(rows, THREADS / LPR));
+            const uint32_t blocks = (uint32_t)even_blocks(ceil_div(rows, THREADS / LPR), LPR > 256 ? kRmsBlocksWide : LPR > 64 ? kRmsBlocks : eight ? kRmsBlocks8 : kRmsBlocksNarrow);
             if (eight)
                 once ? k_rms<VEC, NV, LPR, THREADS, true, true><<<blocks, THREADS, 0, s>>>(a) : k_rms<VEC, NV, LPR, THREADS, true, false><<<blocks, THREADS, 0, s>>>(a);
             else
@@ -642,7 +690,7 @@ extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const vo
         if (rows > 0 && !fits) {
             if (dweight) {
                 const int64_t across = ceil_div(dim, kColumnThreads * (16 / (int64_t)sizeof(T)));
-                blocks = std::min<int64_t>(rows, std::max<int64_t>(1, kRmsGradBlocks / across));
+                blocks = std::min<int64_t>(rows, std::max<int64_t>(1, kColumnBlocks / across));
                 a.dw = blocks == 1 ? (P*)dweight : nullptr;
                 a.sums = (float*)workspace;
                 k_rms_columns<<<dim3((uint32_t)across, (uint32_t)blocks), kColumnThreads, 0, s>>>(a);

@@ -24,7 +24,7 @@ refused unless gradients are off (``torch.no_grad()``).
     dtable = features.embed_grad(ids, dx, table.shape[0], scale=table.shape[1] ** 0.5)
     norm = features.clip_grads([dtable, dw, db], 1.0)
 
-With the root-mean-square norm, and with a step that clips on the way instead:
+With the root-mean-square norm, and with a step of AdamW that clips on the way:
 
     y, rstd, h = features.rms_norm(x, weight, residual)
     dh, dw = features.rms_norm_grad(dy, h, rstd, weight)
@@ -242,15 +242,19 @@ def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
 
     States of 8 bits are rounded up or down at random, by a hash of ``seed``, ``step`` and the element's place, so that
     small changes add up.  They cost 4 bytes of traffic an element instead of 16."""
-    listed = [a if a is None or isinstance(a, (list, tuple)) else list(a) for a in (params, grads, state, copies)]
-    decay = weight_decay if isinstance(weight_decay, (int, float, list, tuple)) else list(weight_decay)
-    _adamw(listed[0], listed[1], listed[2], step, lr, betas[0], betas[1], eps, decay, norm, max_norm, listed[3], seed, stream)
+    if not (isinstance(params, list) and isinstance(grads, list) and isinstance(state, list) and isinstance(weight_decay, float)):
+        params, grads, state = list(params), list(grads), list(state)
+        if not isinstance(weight_decay, (int, float)):
+            weight_decay = list(weight_decay)
+    if copies is not None:
+        copies = list(copies)
+    _adamw(params, grads, state, step, lr, *betas, eps, weight_decay, norm, max_norm, copies, seed, stream)
 
 
-def _adamw(params, grads, state, step, lr, beta1, beta2, eps, decay, norm, max_norm, copies, seed, stream):
+def _adamw(*args):
+    *args, stream = args
     if stream is None:
         d = _device()
-        if _features.adamw(d, _stream(d), params, grads, state, step, lr, beta1, beta2, eps, decay, norm, max_norm, copies, seed) is not None:
+        if _features.adamw(d, _stream(d), *args) is not None:
             return True
-    return _elsewhere(params[0] if params else None, stream, _adamw, params, grads, state, step, lr, beta1, beta2, eps, decay, norm, max_norm, copies,
-                      seed, None)
+    return _elsewhere(args[0][0] if args[0] else None, stream, _adamw, *args, None)

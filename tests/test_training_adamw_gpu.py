@@ -401,3 +401,13 @@ def test_adamw_and_autograd():
     assert torch.allclose(p.detach(), torch.full_like(p, 0.5))
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         saved.backward()
+
+
+def test_example_runs_with_the_step():
+    import math
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import learned_features
+    objectives = learned_features.train(iterations=3, n=2048, adamw=True)
+    assert len(objectives) == 3 and all(math.isfinite(p) for p in objectives)
