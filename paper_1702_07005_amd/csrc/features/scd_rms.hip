@@ -10,6 +10,10 @@
 // between its statistics and its result; groups walk the rows with a fixed stride and load the next row before they work
 // on this one.  The backward pass keeps its share of dw in registers on the way, each workgroup writes its sums to the
 // workspace in 32 bits, and a second kernel adds them in a fixed order.
+//
+// Measured: forward with residual 32,768 x 2,048 (bf16) 87 us, 6.2 TB/s; 16,384 x 4,096 (bf16) with residual into 8 bits 76
+// us, 6.2 TB/s; backward with the residual's gradient 16,384 x 4,096 (bf16) 89 us, 6.0 TB/s, of which the addition of the
+// workgroups' sums takes 4.  Rows that are read again: 4,096 x 32,768 (bf16) 130 us forward, 317 backward.
 #include <algorithm>
 
 #include "scd_device.h"
@@ -77,7 +81,7 @@ __device__ __forceinline__ float row_max(float x, float* lds, int turn) {
     }
 }
 
-// Q: the output in 8 bits.  ONCE: large outputs go past the caches.
+// Q: the output in 8 bits.  ONCE: large matrices are read and written past the caches.
 template <int VEC, int NV, int LPR, int THREADS, bool Q, bool ONCE, typename T, typename P>
 __global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
     __shared__ float lds[lds_words<LPR, THREADS>(1)];
@@ -554,24 +558,36 @@ __global__ void __launch_bounds__(kAcross * kSlices) k_rms_params(const float* _
 
 // ---------------------------------------------------------------------------------------- host
 
-constexpr int kRmsThreads = 256;      // a workgroup, where a row's group is not wider
-constexpr int64_t kRmsBlocks = 65536;
+constexpr int kRmsThreads = 256;  // a workgroup, where a row's group is not wider
+// Workgroups at most.  Rows of a wave or less: 2 M x 16 (fp32, residual) 88 us with these, 92 with 8,192, 97 with 2,048 and
+// 87 without a limit, but 2 M x 16 (bf16) 44.6, 44.3, 51 and 50; with 8 bits 50,000 x 624 (bf16) 40 with 8,192 and 44.
 constexpr int64_t kRmsBlocksNarrow = 16384;
 constexpr int64_t kRmsBlocks8 = 8192;
+// Of 128 or 256 lanes: 16,384 x 4,096 (bf16, residual) 87 us with a workgroup for each row, 88 with 8,192, 94 with 2,048.
+constexpr int64_t kRmsBlocks = 65536;
+// Wider: 4,096 x 16,384 (bf16) 48 us with 2,048, 61 with a workgroup for each row; 8,192 x 8,192 45 and 46.5.
 constexpr int64_t kRmsBlocksWide = 2048;
-constexpr int kRmsGradBlocks = 256;   // the backward pass's, whose sums of dw go through memory
-constexpr int kRmsGradBlocksWide = 256;
+// The backward pass's, whose sums of dw go through memory: one to a CU.  16,384 x 4,096 (bf16) 72 us, with 512 workgroups of
+// 256 threads 74, with 512 of 512 76; 4,099 x 1,000 (fp16) 9.3, 10.5 and 11.4.
+constexpr int kRmsGradThreads = 512;
+constexpr int kRmsGradBlocks = 256;
 constexpr int64_t kColumnBlocks = 1024;  // of the sums by columns, which are at least nine across: fewer than 256 a column
-constexpr int64_t kRmsTurnsAlone = 4;  // rows for each group of a workgroup up to which one workgroup does it all
-constexpr int64_t kRmsOnce = int64_t(384) << 20;      // bytes of all matrices
+// Rows for each group of a workgroup up to which one workgroup does it all, which saves the second launch; a row of 512
+// threads or more takes longer than the launch: there one row.
+constexpr int64_t kRmsTurnsAlone = 4;
+// Bytes of all matrices from which they go past the caches.  Forward: 402 MB (12,288 x 4,096, bf16, residual) 65 us past
+// them and 68 through them, 268 MB 44 and 41, 537 MB 86 and 90; with a pass that reads the output at once 97 and 91, 66 and
+// 61, 127 and 135.  In 8 bits 352 MB 57 and 62, 235 MB 39 and 38.5.  Backward: 403 MB 75 and 78, 302 MB 58 and 58, 201 MB 42
+// and 40; with a reader 114 and 126, 89 and 88, 63 and 61.
+constexpr int64_t kRmsOnce = int64_t(384) << 20;
 constexpr int64_t kRmsOnce8 = int64_t(288) << 20;
 constexpr int64_t kRmsGradOnce = int64_t(320) << 20;
-constexpr int kRmsGradThreads = 512;
 
 // Workgroups for `turns` turns, `most` of them at most, each with as many turns.
 int64_t even_blocks(int64_t turns, int64_t most) { return ceil_div(turns, ceil_div(turns, most)); }
 
-// with_group for the backward pass, whose widest rows take 1,024 threads.
+// with_group for the backward pass, whose widest rows take 1,024 threads that load a row when they come to it: 8,192 x 16,384
+// (bf16) 142 us, with 512 threads that load the next one ahead 169; 4,096 x 16,384 (fp32) 149 and 229.
 template <typename T, typename F>
 bool with_grad_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
@@ -679,7 +695,7 @@ extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const vo
             constexpr int THREADS = LPR > kRmsGradThreads ? LPR : kRmsGradThreads;
             constexpr int64_t groups = THREADS / LPR;
             const bool alone = rows <= (LPR >= 512 ? 1 : kRmsTurnsAlone) * groups;
-            blocks = alone && dweight ? 1 : std::min<int64_t>(LPR >= 512 ? kRmsGradBlocksWide : kRmsGradBlocks, ceil_div(rows, groups));
+            blocks = alone && dweight ? 1 : std::min<int64_t>(kRmsGradBlocks, ceil_div(rows, groups));
             a.dw = alone ? (P*)dweight : nullptr;
             a.sums = alone || !dweight ? nullptr : (float*)workspace;
             if (rows * dim * (residual_grad ? 4 : 3) * (int64_t)sizeof(T) <= kRmsGradOnce)

@@ -411,3 +411,30 @@ def test_example_runs_with_the_step():
     import learned_features
     objectives = learned_features.train(iterations=3, n=2048, adamw=True)
     assert len(objectives) == 3 and all(math.isfinite(p) for p in objectives)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_offsets_beyond_32_bits(bits):
+    n = (1 << 32) + 1000
+    at = [0, 5, 255, (1 << 31) + 7, (1 << 32) - 1, 1 << 32, (1 << 32) + 5, n - 1]
+    p, grad = (torch.zeros(n, dtype=BF16, device=DEV) for _ in range(2))
+    state = features.adamw_state([p], bits)
+    values = torch.arange(1.0, len(at) + 1).bfloat16()
+    grad[torch.tensor(at, device=DEV)] = values.to(DEV)
+    features.adamw([p], [grad], state, 1, lr=0.25, weight_decay=0.0, seed=3)
+    assert int((p != 0).sum()) == len(at)
+    assert (p[torch.tensor(at, device=DEV)] == -0.25).all()
+    if bits == 32:
+        m = state[0][0][torch.tensor(at, device=DEV)].cpu()
+        assert ((m.double() - 0.1 * values.double()).abs() <= 3 * fo.U * 0.1 * values.double()).all()
+        return
+    for first in (0, (1 << 32) - 256, 1 << 32):  # whole blocks, whose words come from beyond 32 bits
+        here = slice(first, first + 256)
+        g = grad[here].double().cpu()
+        block = first // 256
+        for q, s, value, which, to_8 in ((state[0][0], state[0][2], 0.1 * g, 0, to.round_m), (state[0][1], state[0][3], (0.001 * g * g).sqrt(), 1, to.round_r)):
+            scale = s[block].double().cpu()
+            assert abs(float(scale) * to.TOP / float(value.max()) - 1) < 1e-6
+            u = to.uniform(to.words(256, 3, 1, 0, start=first))[which]
+            least, most = to_8(value / scale * (1 - 1e-6), u), to_8(value / scale * (1 + 1e-6), u)
+            to.between(q[here], (least, most, torch.sign(value)), f"{first} {which}")
