@@ -28,8 +28,8 @@ def depth(dim):
 
 def grid(x):
     """The distance of neighbouring values of 8 bits around |x|."""
-    e = torch.frexp(x.abs().clamp(min=2.0 ** -6))[1] - 1  # exact, unlike a logarithm
-    return torch.ldexp(torch.ones_like(x), e - 3)
+    e = x.abs().clamp(min=2.0 ** -6).double().view(torch.int64) >> 52  # the exponent's bits: exact on every device
+    return ((e - 3) << 52).view(torch.float64).to(x.dtype)
 
 
 def stream(x, residual):
@@ -103,9 +103,9 @@ def mix(h):
     return h ^ (h >> 16)
 
 
-def words(n, seed, step, place, start=0):
+def words(n, seed, step, place, start=0, device="cpu"):
     key = mix((mix(seed ^ mix(step & 0xFFFFFFFF)) + place) & 0xFFFFFFFF)
-    at = torch.arange(start, start + n, dtype=torch.int64)
+    at = torch.arange(start, start + n, dtype=torch.int64, device=device)
     return mix((at & 0xFFFFFFFF) ^ ((key + (at >> 32)) & 0xFFFFFFFF))
 
 
@@ -172,7 +172,7 @@ def adamw(p, grad, state, step, lr, betas, eps, decay, norm=None, max_norm=1.0, 
     if not eight:
         out["m"], out["v"] = (m, SLACK * e_m + 2.0 ** -149), (v, SLACK * e_v + 2.0 ** -148)
         return out
-    um, ur = uniform(words(p.numel(), seed, step, place))
+    um, ur = uniform(words(p.numel(), seed, step, place, device=p.device))
     r = v.sqrt()
     e_r = (0.5 * 9 + 1) * U * r
     for name, x, e, u, to in (("m", m, e_m, um, round_m), ("r", r, e_r, ur, round_r)):
@@ -193,7 +193,7 @@ def adamw(p, grad, state, step, lr, betas, eps, decay, norm=None, max_norm=1.0, 
 
 def between(got, want, what=""):
     """Asserts that values of 8 bits are those that the value's bound allows."""
-    least, most, sign = want
+    least, most, sign = (t.cpu() for t in want)
     got = got.detach().cpu().float().double()
     assert not torch.isnan(got).any(), f"{what}: NaN"
     bad = (got.abs() < least) | (got.abs() > most) | (got * sign < 0)

@@ -147,6 +147,40 @@ def test_adamw_large_chunks(bits):
             assert abs(float((m - 0.1 * grad.double()).sum() / off.square().sum().sqrt())) < 6
 
 
+# Enough elements to go past the caches, of every type; a few million are compared.
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("p,g", TYPES)
+def test_adamw_past_the_caches(p, g, bits):
+    gen = torch.Generator(device=DEV).manual_seed(bits)
+    n, most = [13_500_001, 70_001], 1_000_192
+    ps, gs = [torch.randn(k, device=DEV, generator=gen).to(p) for k in n], [(torch.randn(k, device=DEV, generator=gen) * 0.1).to(g) for k in n]
+    state = features.adamw_state(ps, bits)
+    copy = BF16 if p == F32 else None
+    copies = [torch.zeros(k, dtype=BF16, device=DEV) for k in n] if copy else None
+    norm = features.grad_norm(gs)
+    for t in (1, 2):
+        before = [(q.clone(), tuple(s.clone() for s in st)) for q, st in zip(ps, state)]
+        features.adamw(ps, gs, state, t, lr=1e-2, norm=norm, max_norm=3.0, copies=copies, seed=9)
+        for k, (q, st) in enumerate(before):
+            m = min(most, n[k])
+            part = tuple(s[:m] if s.numel() == n[k] else s[:-(-m // to.BLOCK)] for s in st)
+            want = to.adamw(q[:m], gs[k][:m], part, t, 1e-2, BETAS, float(torch.tensor(1e-8)), float(torch.tensor(0.01)), float(norm), 3.0, copy, 9, place=k)
+            want = {name: tuple(w.cpu() for w in v) for name, v in want.items()}
+            fo.close(ps[k][:m], want["param"], "param")
+            if copy:
+                fo.close(copies[k][:m], want["copy"], "copy")
+            if bits == 32:
+                fo.close(state[k][0][:m], want["m"], "m")
+                fo.close(state[k][1][:m], want["v"], "v")
+            else:
+                to.between(state[k][0][:m], want["m"], "m")
+                to.between(state[k][1][:m], want["r"], "r")
+                fo.close(state[k][2][:-(-m // to.BLOCK)], want["m_scale"], "m_scale")
+                fo.close(state[k][3][:-(-m // to.BLOCK)], want["r_scale"], "r_scale")
+            last = slice(n[k] - 5, n[k])
+            assert (ps[k][last] != q[last]).any()
+
+
 def test_adamw_takes_scalars_from_the_gpu():
     g = _gen(9)
     for bits in (32, 8):

@@ -355,3 +355,52 @@ def test_rms_writes_count_as_in_place_operations():
     features.rms_norm_8bit(x, w, out=q)
     features.rms_norm_grad(x, x, stats, w, out=y)
     assert [t._version - b for t, b in zip((x, y, total, q), before)] == [0, 2, 1, 1]
+
+
+# A width for every group of lanes and every type: matrices that go past the caches are copies of a small one, each of which
+# has to lie within the small one's bounds.
+@pytest.mark.parametrize("x,p", PAIRS)
+@pytest.mark.parametrize("dim", [3, 14, 30, 60, 120, 250, 500, 700, 1000, 1500, 2000, 4000, 8000, 16_000])
+def test_rms_norm_widths_past_the_caches(dim, x, p):
+    g = torch.Generator(device=DEV).manual_seed(dim)
+    few = 37
+    small = [torch.randn(few, dim, generator=g, device=DEV).to(x) for _ in range(3)]
+    w = (1 + 0.3 * torch.randn(dim, generator=g, device=DEV)).to(p)
+    copies = -(-int(1.03 * (384 << 20)) // (few * dim * small[0].element_size() * 3))  # of three matrices; four and more are above every limit
+    big = [t.repeat(copies, 1) for t in small]
+
+    def within(got, want, what):
+        value, bound = (t.to(DEV) for t in want)
+        got = got.view(-1, *value.shape)
+        for part in got.split(max(1, 30_000_000 // value.numel())):
+            bad = (part.double() - value).abs() > bound
+            assert not bad.any(), f"{what}: {int(bad.sum())} of {part.numel()} outside their bound"
+
+    host = [t.cpu() for t in small]
+    for res in (False, True):
+        xs = big[0] if res else big[0].repeat(2, 1)  # without a residual, two matrices: twice the rows
+        h = to.stream(host[0], host[1] if res else None)
+        want_y, want_rstd = to.rms_norm(h, w.cpu(), EPS)
+        y, rstd, kept = features.rms_norm(xs, w, big[1] if res else None)
+        within(y, want_y, "y")
+        within(rstd, want_rstd, "rstd")
+        assert torch.equal(kept.view(-1, few, dim), h.to(DEV).expand(kept.shape[0] // few, few, dim))
+        del y
+        for group in (None, 64):
+            q, scale, _, _ = features.rms_norm_8bit(xs, w, big[1] if res else None, group=group)
+            want_q, want_scale = to.rms_norm_8bit(h, w.cpu(), EPS, group)
+            within(q.float(), want_q, f"q {group}")
+            within(scale, want_scale, f"scale {group}")
+            del q
+    _, rstd, _ = features.rms_norm(small[0], w)
+    for res in (False, True):
+        dh, dw = features.rms_norm_grad(big[2], big[0], rstd.repeat(copies), w, big[1] if res else None)
+        want_dh, _ = to.rms_norm_grad(host[2], host[0], rstd.cpu(), w.cpu(), host[1] if res else None, x, p)
+        within(dh, want_dh, "dh")
+        terms = small[2].double() * (small[0].double() * rstd.double()[:, None])
+        # no term takes part in more additions than a lane has rows, and the groups' and workgroups' sums
+        bound = copies * terms.abs().sum(0) * (few * copies / 256 + 64) * 1.05 * fo.U + (1.05 * fo.ROUND[p][0]) * copies * terms.sum(0).abs() + 2.0 ** -24
+        value, largest = copies * terms.sum(0), torch.finfo(p).max
+        over = value.abs() - bound > largest  # sums of 600,000 rows may be beyond fp16: infinite
+        assert torch.equal(torch.isinf(dw), over) and torch.equal(torch.sign(dw)[over], torch.sign(value)[over].to(p))
+        assert ((dw.double() - value).abs() <= bound)[~over].all()
