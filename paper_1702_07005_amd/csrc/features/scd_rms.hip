@@ -586,14 +586,25 @@ constexpr int64_t kRmsGradOnce = int64_t(320) << 20;
 // Workgroups for `turns` turns, `most` of them at most, each with as many turns.
 int64_t even_blocks(int64_t turns, int64_t most) { return ceil_div(turns, ceil_div(turns, most)); }
 
-// with_group for the backward pass, whose widest rows take 1,024 threads that load a row when they come to it: 8,192 x 16,384
-// (bf16) 142 us, with 512 threads that load the next one ahead 169; 4,096 x 16,384 (fp32) 149 and 229.
-template <typename T, typename F>
-bool with_grad_group(int64_t dim, F&& f) {
+// with_group, but with three vectors a lane where two leave a quarter of twice the lanes or more without work: 8,000 x 10,000
+// (bf16) 55 us and 60, 16,384 x 2,560 (fp32, residual) 108 and 121, into 8 bits 16,384 x 2,560 (bf16) 54 and 59; backward in
+// fp32 alone, 16,384 x 2,500 85 and 92, for with 16-bit elements three vectors take registers that leave a SIMD two waves
+// (16,384 x 2,560 57 and 48).  The backward pass's widest rows take 1,024 threads that load a row when they come to it:
+// 8,192 x 16,384 (bf16) 142 us, with 512 threads that load the next one ahead 169; 4,096 x 16,384 (fp32) 149 and 229.
+template <typename T, bool GRAD, typename F>
+bool with_rms_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
     const int64_t vecs = ceil_div(dim, V);
-    if (vecs <= 1024) return with_group<T, true>(dim, f);
-    if (vecs <= 2048)
+    if constexpr (!GRAD || V == 4) {
+        const bool narrow = vecs > 256 && vecs <= 3 * 128, wide = vecs > 512 && vecs <= 3 * 256, widest = vecs > 1024 && vecs <= 3 * 512;
+        if (narrow) f(Int<V>{}, Int<3>{}, Int<128>{});
+        if (wide) f(Int<V>{}, Int<3>{}, Int<256>{});
+        if (widest) f(Int<V>{}, Int<3>{}, Int<512>{});
+        if (narrow || wide || widest) return true;
+    }
+    if (!GRAD || vecs <= 1024)
+        return with_group<T, GRAD>(dim, f);
+    else if (vecs <= 2048)
         f(Int<V>{}, Int<2>{}, Int<1024>{});
     else if constexpr (V == 4) {
         if (vecs > 4096) return false;
@@ -645,7 +656,7 @@ extern "C" int scd_rms_norm(const void* x, int32_t type, int64_t x_stride, const
                               (int32_t)group, (int32_t)(group ? ceil_div(dim, group) : 1), y, y_stride, scale, residual ? (T*)sum : nullptr, sum_stride, rstd};
         const int64_t matrices = rows * dim * (int64_t)sizeof(T) * (residual ? 3 : 1);
         const bool once = eight ? matrices + rows * dim > kRmsOnce8 : matrices + rows * dim * (int64_t)sizeof(T) > kRmsOnce;
-        const bool fits = with_group<T, false>(dim, [&](auto vec, auto nv, auto lpr) {
+        const bool fits = with_rms_group<T, false>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kRmsThreads ? LPR : kRmsThreads;
             const uint32_t blocks = (uint32_t)even_blocks(ceil_div(rows, THREADS / LPR), LPR > 256 ? kRmsBlocksWide : LPR > 64 ? kRmsBlocks : eight ? kRmsBlocks8 : kRmsBlocksNarrow);
@@ -690,7 +701,7 @@ extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const vo
         RmsGradArgs<T, P> a{(const T*)grad, grad_stride, (const T*)h, h_stride, (const T*)residual_grad, residual_stride, rstd, (int32_t)rows,
                             (int32_t)dim, (const P*)weight, (T*)dh, dh_stride, nullptr, nullptr};
         int64_t blocks = 0;  // whose sums go through the workspace
-        const bool fits = rows > 0 && with_grad_group<T>(dim, [&](auto vec, auto nv, auto lpr) {
+        const bool fits = rows > 0 && with_rms_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
             constexpr int THREADS = LPR > kRmsGradThreads ? LPR : kRmsGradThreads;
             constexpr int64_t groups = THREADS / LPR;
