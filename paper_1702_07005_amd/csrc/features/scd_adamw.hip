@@ -27,46 +27,67 @@ namespace scd {
 namespace feat {
 namespace {
 
-constexpr int kSteps = 44;             // tensors a launch: the arguments stay below 4 KB
+constexpr int kSteps = 64;             // tensors a launch, a lane for each: the arguments stay below 4 KB
+constexpr int kSteps8 = 47;            // with states of 8 bits
 constexpr int kStateBlock = 256;       // elements that share a scale
 // A workgroup is one wave, and has one turn.  In this order, what runs at a time lies close together in memory: 354 M weights
 // 2,011 us with 2,048 workgroups of 256 threads that each take a run of chunks, 1,692 with a workgroup of 256 for each 1,024
 // elements, 1,640 with one of 64 for each 256 (states of 32 bits); with 8 bits 1,191, 980 and 960.
 constexpr int kStepThreads = 64;
 constexpr int64_t kStepChunk = 256;    // elements of a workgroup, 32 bits
+// There a tensor's chunks begin where its states' lines do, the first of them up to this many elements early: tensors at odd
+// places of one buffer (26 layers of width 897, 107 M weights in all, fp32 gradients, bf16 copies) 515 us, without this 708,
+// of width 896 502.
+constexpr uint32_t kStepLine = 64;
+// With 8 bits, where the blocks are fixed, as many consecutive chunks go to one XCD, so that few lines are shared between two:
+// 354 M weights 914 us, 966 without; 945 with 256, 983 with 16.  With 32 bits 1,693 with 64 and 1,555 without.
+constexpr uint32_t kTogether8 = 64;
+constexpr uint32_t kXcds = 8;
 constexpr int64_t kStepChunk8 = 512;   // and 8
 constexpr int64_t kStepBlocks = kMaxThreads / kStepThreads;  // workgroups of a launch at most
 constexpr int64_t kStepMost = int64_t(1) << 39;              // elements of a call: chunk numbers stay below 2^32
 // Calls that read and write this much go past the caches.  On states that other work has displaced: 10 M weights (280 MB, 32
 // bits) 47 us past them and 54 through them, 6 M (168 MB) 30 and 35, 1 M (28 MB) 7.1 and 7.2; with a pass that reads the
-// copy at once 60 and 62, 40 and 40, 10.8 and 10.2; but on states that the caches still hold 6 M take 29 and 27.
+// copy at once 60 and 62, 40 and 40, 10.8 and 10.2; but on states that the caches still hold 6 M take 29 and 27.  Not where
+// the accesses are not of whole lines, which are then read and written twice: with 8 bits and width 897 348 us through the
+// caches, 387 past them (bf16 gradients), of width 896 324 and 290.
 constexpr int64_t kStepOnce = int64_t(128) << 20;
 // LDS that a workgroup of states in 32 bits asks for and does not use, so that sixteen are on a CU at a time, four to a SIMD:
 // with fewer bytes in flight the memory gives more.  354 M weights: 32 waves 1,645 us, 20 1,556, 16 1,548, 14 1,558, 12
 // 1,597, 8 1,976.  States of 8 bits, whose waves compute as long as they wait, take as many as their registers allow.
 constexpr int kStepLds = 10240;
 
-struct Step {
+struct Step32 {
     void* p;
     const void* g;
     void* m;
     void* v;
-    float* ms;
-    float* vs;
     void* copy;
     int64_t n;
-    uint32_t place;  // in the call's list
     float decay;
-    uint8_t pt, gt, ct, st;
-    uint32_t pad_;
+    uint8_t pt, gt, ct, pad_;
 };
+struct Step8 {
+    void* p;
+    const void* g;
+    void* m;
+    void* v;
+    void* copy;
+    int64_t n;
+    float decay;
+    uint8_t pt, gt, ct, pad_;
+    float* ms;
+    float* vs;
+    uint64_t place;  // in the call's list
+};
+template <bool EIGHT>
 struct StepArgs {
-    Step s[kSteps];
-    uint32_t first[kSteps];  // number of chunks before each tensor's
+    static constexpr int kMost = EIGHT ? kSteps8 : kSteps;
+    std::conditional_t<EIGHT, Step8, Step32> s[kMost];
+    uint32_t first[kMost];  // number of chunks before each tensor's
     uint32_t count;
     uint32_t chunks;
-    uint32_t chunk;  // elements of a chunk
-    uint32_t from;   // the launch's first chunk
+    uint32_t from;  // the launch's first chunk
     uint32_t seed;
     const float* lr_dev;
     const int64_t* step_dev;
@@ -78,8 +99,14 @@ struct StepArgs {
     float eps, max_norm;
     float rate, root;  // where neither lr nor step are on the GPU
 };
-static_assert(sizeof(StepArgs) <= 4096, "kernel arguments");
-static_assert(kSteps <= 64, "a lane for each tensor");
+static_assert(sizeof(StepArgs<false>) <= 4096 && sizeof(StepArgs<true>) <= 4096, "kernel arguments");
+static_assert(kSteps <= 64 && kSteps8 <= 64, "a lane for each tensor");
+
+// The elements by which a tensor's first chunk begins early.
+template <bool EIGHT>
+__host__ __device__ inline uint32_t early(const void* m) {
+    return EIGHT ? 0 : (uint32_t)((uintptr_t)m / 4 % kStepLine);
+}
 
 // What all elements of a launch share.
 struct Common {
@@ -90,7 +117,8 @@ struct Common {
     uint32_t key;
 };
 
-__device__ __forceinline__ Common common_of(const StepArgs& a) {
+template <bool EIGHT>
+__device__ __forceinline__ Common common_of(const StepArgs<EIGHT>& a) {
     Common c;
     c.b1 = a.b1;
     c.b2 = a.b2;
@@ -118,9 +146,10 @@ __device__ __forceinline__ Common common_of(const StepArgs& a) {
 }
 
 // The tensor that holds a chunk: a lane looks at each.
-__device__ __forceinline__ uint32_t tensor_of(const StepArgs& a, uint32_t chunk) {
+template <bool EIGHT>
+__device__ __forceinline__ uint32_t tensor_of(const StepArgs<EIGHT>& a, uint32_t chunk) {
     const uint32_t lane = threadIdx.x % 64;
-    const uint64_t before = __ballot(lane < a.count && a.first[min(lane, (uint32_t)kSteps - 1)] <= chunk);
+    const uint64_t before = __ballot(lane < a.count && a.first[min(lane, (uint32_t)a.kMost - 1)] <= chunk);
     return (uint32_t)__builtin_popcountll(before) - 1;
 }
 
@@ -153,7 +182,7 @@ __device__ __forceinline__ void put_4(uint8_t* p, uint32_t w) {
 
 // V elements from the i-th on, states in 32 bits.
 template <bool ONCE, int V, typename P, typename G>
-__device__ __forceinline__ void step_32(const Common& c, const Step& s, float keep, int64_t i) {
+__device__ __forceinline__ void step_32(const Common& c, const Step32& s, float keep, int64_t i) {
     float p[V], g[V], m[V], v[V];
     fetch_vec<ONCE>((const P*)s.p + i, p);
     fetch_vec<ONCE>((const G*)s.g + i, g);
@@ -172,15 +201,16 @@ __device__ __forceinline__ void step_32(const Common& c, const Step& s, float ke
     if (s.copy) store_copy<ONCE>(s.copy, s.ct, i, p);
 }
 
+// A wave's chunk, four elements a lane; one that the tensor fills in part goes element by element.
 template <bool ONCE, typename P, typename G>
-__device__ __forceinline__ void chunk_32(const Common& c, const Step& s, int64_t at, int32_t n) {
+__device__ __forceinline__ void chunk_32(const Common& c, const Step32& s, int64_t at) {
+    static_assert(kStepChunk == kStepThreads * 4, "one turn");
     const float keep = (float)(1.0 - c.lr * (double)s.decay);
-    for (int32_t i = threadIdx.x * 4; i < n; i += kStepThreads * 4) {
-        if (i + 4 <= n) {
-            step_32<ONCE, 4, P, G>(c, s, keep, at + i);
-        } else {
-            for (int32_t k = i; k < n; ++k) step_32<false, 1, P, G>(c, s, keep, at + k);
-        }
+    if (at >= 0 && at + kStepChunk <= s.n) {
+        step_32<ONCE, 4, P, G>(c, s, keep, at + threadIdx.x * 4);
+    } else {
+        const int64_t end = min(at + kStepChunk, s.n);
+        for (int64_t k = max(at, (int64_t)0) + threadIdx.x; k < end; k += kStepThreads) step_32<false, 1, P, G>(c, s, keep, k);
     }
 }
 
@@ -267,7 +297,7 @@ __device__ __forceinline__ uint32_t random_r4(const float* x, const uint32_t* wo
 // A wave's chunk: two blocks of a tensor, from the `at`-th element on, `n` elements of them.  Half of the wave takes a block, each lane four
 // elements of its first half and four of its second, so that every access of the wave is to whole lines.
 template <bool ONCE, typename P, typename G>
-__device__ __forceinline__ void blocks_8(const StepArgs& a, const Step& s, int64_t at, int32_t n) {
+__device__ __forceinline__ void blocks_8(const StepArgs<true>& a, const Step8& s, int64_t at, int32_t n) {
     constexpr int V = 8, kApart = kStateBlock / 2;
     const int32_t lane = threadIdx.x % 64, begin = lane / 32 * kStateBlock, i = begin + lane % 32 * 4;
     const int64_t from = at + i, block = (at + begin) / kStateBlock;
@@ -373,7 +403,7 @@ __device__ __forceinline__ void blocks_8(const StepArgs& a, const Step& s, int64
     }
     const float to_m = e4m3_scale(__uint_as_float(most_m)), to_r = e4m3_scale(__uint_as_float(most_r));
     const float im = inverse(to_m), ir = inverse(to_r);
-    const uint32_t key = murmur_fmix32(c.key + s.place) + (uint32_t)((uint64_t)at >> 32);
+    const uint32_t key = murmur_fmix32(c.key + (uint32_t)s.place) + (uint32_t)((uint64_t)at >> 32);
 #pragma unroll
     for (int k = 0; k < V / 4; ++k) {
         uint32_t word[4];
@@ -411,19 +441,27 @@ __device__ __forceinline__ void blocks_8(const StepArgs& a, const Step& s, int64
 
 // EIGHT: the tensors of a launch have states in 8 bits.  ONCE: past the caches.
 template <bool EIGHT, bool ONCE>
-__global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs a) {
+__global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs<EIGHT> a) {
     static_assert(kStepChunk8 == 2 * kStateBlock, "one turn");
     Common c;
     if constexpr (!EIGHT) c = common_of(a);
-    const uint32_t chunk = a.from + blockIdx.x, k = tensor_of(a, chunk);
-    const Step& s = a.s[k];
-    const int64_t at = (int64_t)(chunk - a.first[k]) * a.chunk;
-    const int32_t n = (int32_t)min((int64_t)a.chunk, s.n - at);
+    uint32_t chunk = blockIdx.x;
+    if constexpr (EIGHT) {
+        constexpr uint32_t kTurn = kXcds * kTogether8;
+        if (chunk < gridDim.x / kTurn * kTurn) {  // workgroup b runs on XCD b mod 8
+            const uint32_t on = chunk / kXcds;
+            chunk = on / kTogether8 * kTurn + chunk % kXcds * kTogether8 + on % kTogether8;
+        }
+    }
+    chunk += a.from;
+    const uint32_t k = tensor_of(a, chunk);
+    const auto& s = a.s[k];
+    const int64_t at = (int64_t)(chunk - a.first[k]) * (EIGHT ? kStepChunk8 : kStepChunk) - early<EIGHT>(s.m);
     const auto step = [&](auto p, auto g) {
         if constexpr (EIGHT)
-            blocks_8<ONCE, decltype(p), decltype(g)>(a, s, at, n);
+            blocks_8<ONCE, decltype(p), decltype(g)>(a, s, at, (int32_t)min(kStepChunk8, s.n - at));
         else
-            chunk_32<ONCE, decltype(p), decltype(g)>(c, s, at, n);
+            chunk_32<ONCE, decltype(p), decltype(g)>(c, s, at);
     };
     if (s.pt == SCD_F32)
         s.gt == SCD_F32 ? step(float{}, float{}) : s.gt == SCD_BF16 ? step(float{}, bf16{}) : step(float{}, f16{});
@@ -431,6 +469,68 @@ __global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs a) {
         s.gt == SCD_F32 ? step(bf16{}, float{}) : step(bf16{}, bf16{});
     else
         s.gt == SCD_F32 ? step(f16{}, float{}) : step(f16{}, f16{});
+}
+
+// Whether lines of all arrays of a tensor begin with its whole chunks.
+template <bool EIGHT>
+bool whole_lines(const scd_adamw_span_t& t) {
+    const int64_t at = -(int64_t)early<EIGHT>(t.m), state = EIGHT ? 1 : 4;
+    const auto place = [at](const void* p, int64_t bytes) { return (uint64_t)(uintptr_t)p + (uint64_t)(at * bytes); };
+    return ((place(t.param, type_bytes(t.param_type)) | place(t.grad, type_bytes(t.grad_type)) | place(t.m, state) | place(t.v, state) |
+             (t.copy ? place(t.copy, 2) : 0)) % 64) == 0;
+}
+
+// The launches for the tensors with states of one kind; with `once`, those past the caches and those through them.
+template <bool EIGHT, bool ONCE>
+void launch_steps(const scd_adamw_span_t* spans, int64_t count, const scd_adamw_t& o, bool once, hipStream_t stream) {
+    StepArgs<EIGHT> a;
+    a.seed = o.seed;
+    a.lr_dev = o.lr_dev;
+    a.step_dev = o.step_dev;
+    a.norm_dev = o.norm_dev;
+    a.lr = o.lr;
+    a.log_b1 = std::log(o.beta1);
+    a.log_b2 = std::log(o.beta2);
+    a.b1 = (float)o.beta1;
+    a.b2 = (float)o.beta2;
+    a.a1 = (float)(1.0 - o.beta1);
+    a.a2 = (float)(1.0 - o.beta2);
+    a.eps = (float)o.eps;
+    a.max_norm = o.max_norm;
+    a.step = o.step;
+    a.rate = (float)(o.lr / -std::expm1((double)o.step * a.log_b1));
+    a.root = (float)(1.0 / std::sqrt(-std::expm1((double)o.step * a.log_b2)));
+    for (int64_t i = 0; i < count;) {
+        a.count = 0;
+        a.chunks = 0;
+        for (; i < count && a.count < a.kMost; ++i) {
+            const scd_adamw_span_t& t = spans[i];
+            if (t.n == 0 || (t.state_type == SCD_E4M3) != EIGHT || (once && whole_lines<EIGHT>(t)) != ONCE) continue;
+            auto& s = a.s[a.count];
+            s.p = t.param;
+            s.g = t.grad;
+            s.m = t.m;
+            s.v = t.v;
+            s.copy = t.copy;
+            s.n = t.n;
+            s.decay = t.weight_decay;
+            s.pt = (uint8_t)t.param_type;
+            s.gt = (uint8_t)t.grad_type;
+            s.ct = (uint8_t)t.copy_type;
+            if constexpr (EIGHT) {
+                s.ms = t.m_scale;
+                s.vs = t.v_scale;
+                s.place = (uint64_t)i;
+            }
+            a.first[a.count++] = a.chunks;
+            a.chunks += (uint32_t)ceil_div(t.n + early<EIGHT>(t.m), EIGHT ? kStepChunk8 : kStepChunk);
+        }
+        for (int64_t from = 0; from < a.chunks; from += kStepBlocks) {
+            a.from = (uint32_t)from;
+            const uint32_t blocks = (uint32_t)std::min<int64_t>(kStepBlocks, a.chunks - from);
+            k_adamw<EIGHT, ONCE><<<blocks, kStepThreads, EIGHT ? 0 : kStepLds, stream>>>(a);
+        }
+    }
 }
 
 }  // namespace
@@ -463,47 +563,12 @@ extern "C" int scd_adamw(const scd_adamw_span_t* spans, int64_t count, const scd
         bytes += t.n * (2 * type_bytes(t.param_type) + type_bytes(t.grad_type) + (t.state_type == SCD_F32 ? 16 : 4) + (t.copy ? 2 : 0));
     }
     if (total == 0) return SCD_OK;
-    StepArgs a;
-    a.seed = o.seed;
-    a.lr_dev = o.lr_dev;
-    a.step_dev = o.step_dev;
-    a.norm_dev = o.norm_dev;
-    a.lr = o.lr;
-    a.log_b1 = std::log(o.beta1);
-    a.log_b2 = std::log(o.beta2);
-    a.b1 = (float)o.beta1;
-    a.b2 = (float)o.beta2;
-    a.a1 = (float)(1.0 - o.beta1);
-    a.a2 = (float)(1.0 - o.beta2);
-    a.eps = (float)o.eps;
-    a.max_norm = o.max_norm;
-    a.step = o.step;
-    a.rate = (float)(o.lr / -std::expm1((double)o.step * a.log_b1));
-    a.root = (float)(1.0 / std::sqrt(-std::expm1((double)o.step * a.log_b2)));
-    hipStream_t s = (hipStream_t)stream;
     const bool once = bytes >= kStepOnce;
-    for (const bool eight : {false, true}) {
-        a.chunk = (uint32_t)(eight ? kStepChunk8 : kStepChunk);
-        for (int64_t i = 0; i < count;) {
-            a.count = 0;
-            a.chunks = 0;
-            for (; i < count && a.count < kSteps; ++i) {
-                const scd_adamw_span_t& t = spans[i];
-                if (t.n == 0 || (t.state_type == SCD_E4M3) != eight) continue;
-                a.first[a.count] = a.chunks;
-                a.s[a.count++] = Step{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, (uint32_t)i, t.weight_decay, (uint8_t)t.param_type,
-                                      (uint8_t)t.grad_type, (uint8_t)t.copy_type, (uint8_t)t.state_type, 0};
-                a.chunks += (uint32_t)ceil_div(t.n, (int64_t)a.chunk);
-            }
-            for (int64_t from = 0; from < a.chunks; from += kStepBlocks) {
-                a.from = (uint32_t)from;
-                const uint32_t blocks = (uint32_t)std::min<int64_t>(kStepBlocks, a.chunks - from);
-                if (eight)
-                    once ? k_adamw<true, true><<<blocks, kStepThreads, 0, s>>>(a) : k_adamw<true, false><<<blocks, kStepThreads, 0, s>>>(a);
-                else
-                    once ? k_adamw<false, true><<<blocks, kStepThreads, kStepLds, s>>>(a) : k_adamw<false, false><<<blocks, kStepThreads, kStepLds, s>>>(a);
-            }
-        }
+    launch_steps<false, false>(spans, count, o, once, (hipStream_t)stream);
+    launch_steps<true, false>(spans, count, o, once, (hipStream_t)stream);
+    if (once) {
+        launch_steps<false, true>(spans, count, o, once, (hipStream_t)stream);
+        launch_steps<true, true>(spans, count, o, once, (hipStream_t)stream);
     }
     return launched("scd_adamw");
 }

@@ -147,16 +147,28 @@ def test_adamw_large_chunks(bits):
             assert abs(float((m - 0.1 * grad.double()).sum() / off.square().sum().sqrt())) < 6
 
 
-# Enough elements to go past the caches, of every type; a few million are compared.
+# Enough elements to go past the caches, of every type, at the lines' beginnings and at odd places; a million are compared.
+@pytest.mark.parametrize("offset", [0, 3])
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("p,g", TYPES)
-def test_adamw_past_the_caches(p, g, bits):
+def test_adamw_past_the_caches(p, g, bits, offset):
     gen = torch.Generator(device=DEV).manual_seed(bits)
     n, most = [13_500_001, 70_001], 1_000_192
     ps, gs = [torch.randn(k, device=DEV, generator=gen).to(p) for k in n], [(torch.randn(k, device=DEV, generator=gen) * 0.1).to(g) for k in n]
     state = features.adamw_state(ps, bits)
     copy = BF16 if p == F32 else None
     copies = [torch.zeros(k, dtype=BF16, device=DEV) for k in n] if copy else None
+    if offset:
+        wholes = []
+
+        def moved(t):
+            whole = torch.ones(t.numel() + 16, device=DEV).to(t.dtype)
+            whole[offset:offset + t.numel()].copy_(t)
+            wholes.append((whole, t.numel()))
+            return whole[offset:offset + t.numel()]
+
+        ps, gs, state = [moved(t) for t in ps], [moved(t) for t in gs], [tuple(moved(t) for t in st) for st in state]
+        copies = [moved(t) for t in copies] if copy else None
     norm = features.grad_norm(gs)
     for t in (1, 2):
         before = [(q.clone(), tuple(s.clone() for s in st)) for q, st in zip(ps, state)]
@@ -179,6 +191,8 @@ def test_adamw_past_the_caches(p, g, bits):
                 fo.close(state[k][3][:-(-m // to.BLOCK)], want["r_scale"], "r_scale")
             last = slice(n[k] - 5, n[k])
             assert (ps[k][last] != q[last]).any()
+    if offset:
+        assert all((w[:offset].float() == 1).all() and (w[offset + m:].float() == 1).all() for w, m in wholes)
 
 
 def test_adamw_takes_scalars_from_the_gpu():
