@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
                     sum.t[i] = (T)(h[j][i] + (float)more[j].t[i]);
                     h[j][i] = (float)sum.t[i];
                 }
-                if (here && col.skip[j] < VEC) put_vec<ONCE>(a.sum + r * a.sstride + col.at[j], h[j]);
+                if (LPR <= 64 && here && col.skip[j] < VEC) put_vec<ONCE>(a.sum + r * a.sstride + col.at[j], h[j]);
             }
         }
         if (r0 + step < a.rows) fetch(r + step);
@@ -137,6 +137,13 @@ __global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
             for (int i = 0; i < VEC; ++i) s[0] += i >= col.skip[j] ? h[j][i] * h[j][i] : 0.0f;
         group_sums<LPR, THREADS, 1>(s, lds, turn);
         turn ^= 1;
+        // Only now has every wave of a wider group read the row, whose last vector begins early, on columns that another wave
+        // may have; and the sum may take an input's place.  (8,192 x 8,191, bf16, 110 us so and 107 with the sum written above;
+        // in a group of one wave 32,768 x 2,048 would take 88 so and takes 87.)
+        if (LPR > 64 && a.res && here)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (col.skip[j] < VEC) put_vec<ONCE>(a.sum + r * a.sstride + col.at[j], h[j]);
         const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
         float most = 0.0f, part[NV];
 #pragma unroll

@@ -191,6 +191,29 @@ def test_rms_norm_without_weight_in_views_and_in_place(dim):
         fo.close(a, b, what)
 
 
+# The row's last vector, which begins early, is in another wave than the vector whose columns it overlaps.
+@pytest.mark.parametrize("x,dim", [(BF16, 2049), (BF16, 2563), (BF16, 4097), (BF16, 12_289), (F32, 1025), (F32, 2050), (F32, 5123), (F32, 16_129)], ids=str)
+def test_rms_norm_in_place_with_the_last_vector_in_another_wave(x, dim):
+    g, rows = _gen(dim), 301
+    a, res, dy, more = (_rows_of_sizes(g, rows, dim, x).to(DEV) for _ in range(4))
+    w = (1 + _normal(g, dim, std=0.3)).to(x).to(DEV)
+    y, rstd, h = features.rms_norm(a, w, res)
+    q, scale, _, _ = features.rms_norm_8bit(a, w, res)
+    dh, dw = features.rms_norm_grad(dy, h, rstd, w, more)
+    for out, total in ((0, 1), (1, 0)):
+        place = [a.clone(), res.clone()]
+        got = features.rms_norm(place[0], w, place[1], out=place[out], sum_out=place[total])
+        assert torch.equal(place[out], y) and torch.equal(place[total], h) and torch.equal(got[1], rstd)
+    for k in (0, 1):
+        place = [a.clone(), res.clone()]
+        got = features.rms_norm_8bit(place[0], w, place[1], sum_out=place[k])
+        assert torch.equal(got[0].float(), q.float()) and torch.equal(got[1], scale) and torch.equal(place[k], h)
+    for k in range(3):
+        place = [dy.clone(), h.clone(), more.clone()]
+        got = features.rms_norm_grad(place[0], place[1], rstd, w, place[2], out=place[k])
+        assert torch.equal(place[k], dh) and torch.equal(got[1], dw)
+
+
 def test_rms_norm_hard_rows():
     # Zeros, rows far from one and rows that hold an infinity or a NaN, which do not touch the others.
     g = _gen(3)
