@@ -14,8 +14,8 @@
 // becomes 0, where m over it would be without bound.  The random numbers are a hash of seed, step, tensor and element.
 //
 // Measured: 354 M weights (fp32, gradients and copies in bf16) 1,543 us with states of 32 bits, 6.4 TB/s of the 9.9 GB that
-// it cannot do without, and 964 us with 8, 5.9 TB/s of 5.7 GB, where the arithmetic (78 instructions an element) keeps the
-// SIMDs busy for two thirds of that time; 11 tensors of 160,000 weights in all 4.3 and 5.5 us on the GPU.
+// it cannot do without, and 909 us with 8, 6.3 TB/s of 5.7 GB, where the arithmetic (78 instructions an element) keeps the
+// SIMDs busy for two thirds of that time; 11 tensors of 160,000 weights in all 3.8 and 4.7 us on the GPU.
 #include <algorithm>
 #include <cmath>
 
@@ -294,8 +294,8 @@ __device__ __forceinline__ uint32_t random_r4(const float* x, const uint32_t* wo
     return out;
 }
 
-// A wave's chunk: two blocks of a tensor, from the `at`-th element on, `n` elements of them.  Half of the wave takes a block, each lane four
-// elements of its first half and four of its second, so that every access of the wave is to whole lines.
+// A wave's chunk: two blocks of a tensor, from the `at`-th element on, `n` elements of them.  Half of the wave takes a block,
+// each lane four elements of its first half and four of its second, so that every access of the wave is to whole lines.
 template <bool ONCE, typename P, typename G>
 __device__ __forceinline__ void blocks_8(const StepArgs<true>& a, const Step8& s, int64_t at, int32_t n) {
     constexpr int V = 8, kApart = kStateBlock / 2;
@@ -331,8 +331,8 @@ __device__ __forceinline__ void blocks_8(const StepArgs<true>& a, const Step8& s
         }
     }
     const float ms = there ? s.ms[block] : 0.0f, rs = there ? s.vs[block] : 0.0f;
-    // Only now, with the elements on their way, what all of them share: with step and learning rate on the GPU 354 M weights
-    // take 954 us so and 1,025 with this first.  (States of 32 bits 1,550 with it first and 1,620 so.)
+    // Only now, with the elements on their way, what all of them share: 354 M weights take 912 us so and 932 with this first,
+    // with step and learning rate on the GPU 955 and 1,002.  (States of 32 bits 1,546 with it first and 1,620 so.)
     const Common c = common_of(a);
     const float keep = (float)(1.0 - c.lr * (double)s.decay);
 #pragma unroll
