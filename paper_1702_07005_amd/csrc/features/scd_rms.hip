@@ -596,8 +596,11 @@ int64_t even_blocks(int64_t turns, int64_t most) { return ceil_div(turns, ceil_d
 // with_group, but with three vectors a lane where two leave a quarter of twice the lanes or more without work: 8,000 x 10,000
 // (bf16) 55 us and 60, 16,384 x 2,560 (fp32, residual) 108 and 121, into 8 bits 16,384 x 2,560 (bf16) 54 and 59; backward in
 // fp32 alone, 16,384 x 2,500 85 and 92, for with 16-bit elements three vectors take registers that leave a SIMD two waves
-// (16,384 x 2,560 57 and 48).  The backward pass's widest rows take 1,024 threads that load a row when they come to it:
-// 8,192 x 16,384 (bf16) 142 us, with 512 threads that load the next one ahead 169; 4,096 x 16,384 (fp32) 149 and 229.
+// (16,384 x 2,560 57 and 48).  There groups of as many waves as two vectors a lane need: with the residual's gradient 16,384 x
+// 5,120 121 and 129, 8,000 x 10,000 108 and 119, 8,192 x 12,288 116 and 128 (bf16); but of fourteen waves 4,096 x 14,336 89
+// and 78, and forward or in fp32 no width gains by it.  The backward pass's widest rows take 1,024 threads that load a row
+// when they come to it: 8,192 x 16,384 (bf16) 142 us, with 512 threads that load the next one ahead 169; 4,096 x 16,384
+// (fp32) 149 and 229.
 template <typename T, bool GRAD, typename F>
 bool with_rms_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
@@ -608,6 +611,14 @@ bool with_rms_group(int64_t dim, F&& f) {
         if (wide) f(Int<V>{}, Int<3>{}, Int<256>{});
         if (widest) f(Int<V>{}, Int<3>{}, Int<512>{});
         if (narrow || wide || widest) return true;
+    } else if (vecs > 512) {
+        const int64_t waves = ceil_div(vecs, 128);
+        if (waves == 5) f(Int<V>{}, Int<2>{}, Int<320>{});
+        if (waves == 6) f(Int<V>{}, Int<2>{}, Int<384>{});
+        if (waves == 7) f(Int<V>{}, Int<2>{}, Int<448>{});
+        if (waves == 9 || waves == 10) f(Int<V>{}, Int<2>{}, Int<640>{});
+        if (waves == 11 || waves == 12) f(Int<V>{}, Int<2>{}, Int<768>{});
+        if (waves <= 12 && waves != 8) return true;
     }
     if (!GRAD || vecs <= 1024)
         return with_group<T, GRAD>(dim, f);
@@ -710,7 +721,7 @@ extern "C" int scd_rms_norm_grad(const void* grad, int64_t grad_stride, const vo
         int64_t blocks = 0;  // whose sums go through the workspace
         const bool fits = rows > 0 && with_rms_group<T, true>(dim, [&](auto vec, auto nv, auto lpr) {
             constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, LPR = decltype(lpr)::value;
-            constexpr int THREADS = LPR > kRmsGradThreads ? LPR : kRmsGradThreads;
+            constexpr int THREADS = LPR > kRmsGradThreads ? LPR : kRmsGradThreads / LPR * LPR;
             constexpr int64_t groups = THREADS / LPR;
             const bool alone = rows <= (LPR >= 512 ? 1 : kRmsTurnsAlone) * groups;
             blocks = alone && dweight ? 1 : std::min<int64_t>(kRmsGradBlocks, ceil_div(rows, groups));

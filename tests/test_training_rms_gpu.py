@@ -18,7 +18,7 @@ PAIRS = [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)]
 EPS = float(torch.tensor(1e-6))
 # Both sides of every group of lanes: one vector a lane from 4 to 64, two to four in a wave, two or four waves and more, and
 # rows that are read again.
-DIMS = [1, 3, 4, 7, 8, 9, 16, 31, 32, 33, 63, 65, 127, 129, 255, 257, 511, 513, 777, 1025, 1536, 1540, 2049, 2500, 3077, 4097, 5000, 6150, 8193, 10_001, 12_300,
+DIMS = [1, 3, 4, 7, 8, 9, 16, 31, 32, 33, 63, 65, 127, 129, 255, 257, 511, 513, 777, 1025, 1536, 1540, 2049, 2500, 3077, 4097, 5000, 6000, 6150, 8193, 10_001, 12_000, 12_300,
         16_384, 16_385, 40_001]
 
 
@@ -384,7 +384,7 @@ def test_rms_writes_count_as_in_place_operations():
 # A width for every group of lanes and every type: matrices that go past the caches are copies of a small one, each of which
 # has to lie within the small one's bounds.
 @pytest.mark.parametrize("x,p", PAIRS)
-@pytest.mark.parametrize("dim", [3, 14, 30, 60, 120, 250, 500, 700, 1000, 1500, 2000, 2500, 4000, 5000, 8000, 10_000, 16_000])
+@pytest.mark.parametrize("dim", [3, 14, 30, 60, 120, 250, 500, 700, 1000, 1500, 2000, 2500, 4000, 5000, 6000, 7000, 8000, 10_000, 12_000, 16_000])
 def test_rms_norm_widths_past_the_caches(dim, x, p):
     g = torch.Generator(device=DEV).manual_seed(dim)
     few = 37
