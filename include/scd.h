@@ -519,8 +519,8 @@ typedef struct {
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
  * Parameters move by m and v in 32 bits, before these are rounded; a NaN norm makes f NaN, an infinite one 0, as in
  * scd_clip_grads, so that with norm_dev the gradients need not be written clipped.
- * States of 8 bits: the scales are max(largest / 448, 2^-126) of the block's finite |m| and sqrt(v), others become NaN; m / m_scale goes
- * to one of its neighbours in 8 bits with probabilities that keep its mean, sqrt(v) / v_scale with those that keep the
+ * States of 8 bits: the scales are max(largest / 448, 2^-126) of the block's finite |m| and sqrt(v), others become NaN; m /
+ * m_scale goes to one of its neighbours in 8 bits with probabilities that keep its mean, sqrt(v) / v_scale with those that keep the
  * mean of its square, but away from 0.  With fmix32 the finaliser of MurmurHash3, element i of the k-th tensor takes
  *   word = fmix32(low 32 bits of i xor (fmix32(fmix32(seed xor fmix32(low 32 bits of t)) + k) + high 32 bits of i)),
  * and goes away from 0 where (word mod 2^16 + 1/2) / 2^16 (m), (word / 2^16 + 1/2) / 2^16 (sqrt(v); word / 2^16 without
