@@ -226,18 +226,6 @@ __device__ __forceinline__ void next_moments(const Common& c, float g, float m0,
     v = c.b2 * (r0 * r0) + c.a2 * (g * g);
 }
 
-// 1 / scale, rounded once: the instruction's result is a unit off at most, and the remainder corrects it.
-__device__ __forceinline__ float inverse(float scale) {
-    const float q = __builtin_amdgcn_rcpf(scale);
-    return fmaf(fmaf(-q, scale, 1.0f), q, q);
-}
-
-// x / scale, rounded once: the product with the (rounded) inverse is off by two units at most, and the remainder corrects it.
-__device__ __forceinline__ float scaled(float x, float scale, float inverse) {
-    const float q = x * inverse;
-    return fmaf(fmaf(-q, scale, x), inverse, q);
-}
-
 // sqrt(v), rounded once, of 0 or v >= 2^-96.  The instruction's result s is a unit off at most; with its neighbour d below, s d
 // is the square of the point between them but for a quarter of a unit squared, so that v <= s d says that d is nearer.
 __device__ __forceinline__ float root(float v) {

@@ -3,7 +3,7 @@
 //
 // Forward: h = x + residual, rounded to the elements' type; r = 1/sqrt(mean h^2 + eps), y = h r w.  The norm is of the
 // rounded h, which the caller keeps: the gradient reads it, and is that of the values that were used.
-// In 8 bits: q = y / s rounded once from 32 bits, s = max |y| / 448 over the row or over groups of its columns.
+// In 8 bits: q = y / s in 32 bits, rounded, s = max |y| / 448 over the row or over groups of its columns.
 // Backward, n = h r, g = dy w:  dh = r (g - n mean(g n)) (+ the residual's gradient), dw = sum_rows dy n.
 //
 // All are bound by memory: every matrix is read or written once.  A row stays in the registers of a group of lanes
@@ -81,9 +81,13 @@ __device__ __forceinline__ float row_max(float x, float* lds, int turn) {
     }
 }
 
+// Waves a SIMD that registers are left for: in 8 bits three vectors of 16-bit elements would take two more than four waves have
+// (32,768 x 2,560, bf16, residual, 97 us with four and 106 with three).
+constexpr int rms_waves(int elems, int lpr, int threads, bool q) { return q && elems == 24 && lpr > 64 && threads == 256 ? 4 : 1; }
+
 // Q: the output in 8 bits.  ONCE: large matrices are read and written past the caches.
 template <int VEC, int NV, int LPR, int THREADS, bool Q, bool ONCE, typename T, typename P>
-__global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
+__global__ void __launch_bounds__(THREADS, rms_waves(VEC * NV, LPR, THREADS, Q)) k_rms(RmsArgs<T, P> a) {
     __shared__ float lds[lds_words<LPR, THREADS>(1)];
     constexpr int kGroups = THREADS / LPR;
     const int32_t lane = threadIdx.x % LPR;
@@ -159,24 +163,21 @@ __global__ void __launch_bounds__(THREADS) k_rms(RmsArgs<T, P> a) {
             if (Q) most = fmaxf(most, part[j]);
         }
         if constexpr (Q) {
-            float scale = 0.0f, to = 0.0f;
             if (a.group == 0) {
-                scale = e4m3_scale(row_max<LPR, THREADS>(most, lds, turn));
+                const float scale = e4m3_scale(row_max<LPR, THREADS>(most, lds, turn));
                 turn ^= 1;
-                to = 1.0f / scale;
                 if (here && lane == 0) a.scale[r] = scale;
+                divide(h, scale);
             }
             const int lanes = min(a.group / VEC, LPR);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if (a.group) {
-                    scale = e4m3_scale(group_max<(LPR < 32 ? LPR : 32)>(part[j], lanes));
-                    to = 1.0f / scale;
+                    const float scale = e4m3_scale(group_max<(LPR < 32 ? LPR : 32)>(part[j], lanes));
                     const int32_t c = (lane + j * LPR) * VEC;
                     if (here && c < a.dim && c % a.group == 0) a.scale[r * a.scales + c / a.group] = scale;
+                    divide(h[j], scale);
                 }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) h[j][i] *= to;
                 if (here && col.skip[j] < VEC) store_e4m3<VEC>((uint8_t*)a.y + r * a.ystride + col.at[j], h[j], col.skip[j]);
             }
         } else if (here) {
@@ -300,9 +301,7 @@ __global__ void __launch_bounds__(kWideThreads) k_rms_wide(RmsArgs<T, P> a) {
                         const int32_t first = c + u * kApart;
                         if (first < a.dim && first % a.group == 0) a.scale[r * a.scales + first / a.group] = scale;
                     }
-                    const float to = 1.0f / scale;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) y[i] *= to;
+                    divide(y, scale);
                     if (col.skip[u] < V) store_e4m3<V>(q + col.at[u], y, col.skip[u]);
                 });
             }
