@@ -37,7 +37,7 @@ __device__ __forceinline__ float scaled(float x, float scale, float inverse) {
 // Vectors of a lane by their scale.  Below 2^-64 both are multiplied by 2^64 first, so that the remainder of a quotient that 8
 // bits tell from 0 is a number of 32 bits; an infinite scale gives 0 or NaN.  16,384 x 4,096 (bf16) into 8 bits with a scale
 // for each row takes 49 us so, 56 with a division where one is small or infinite (8 registers more), and 47 multiplied by the
-// inverse, which is one rounding more, 47.
+// inverse, which is one rounding more.
 template <int NV, int V>
 __device__ __forceinline__ void divide(float (&x)[NV][V], float scale) {
     constexpr float kSmall = 0x1p-64f;
