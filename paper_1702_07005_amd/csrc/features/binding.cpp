@@ -464,7 +464,8 @@ PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
                        eight ? static_cast<float*>(scale.data_ptr()) : nullptr, group, h.data, h.stride, static_cast<float*>(rstd.data_ptr()), c.stream));
     if (c.given(4)) written(y);
     if (c.given(5)) written(sum);
-    PyObject* const kept = sum.defined() ? THPVariable_Wrap(sum) : Py_NewRef(c.args[0]);
+    // x is h, but not where it holds y now.
+    PyObject* const kept = sum.defined() ? THPVariable_Wrap(sum) : o.data == r.data && r.n > 0 ? none() : Py_NewRef(c.args[0]);
     if (eight) return Py_BuildValue("(NNNN)", THPVariable_Wrap(y), THPVariable_Wrap(scale), THPVariable_Wrap(rstd), kept);
     return Py_BuildValue("(NNN)", THPVariable_Wrap(y), THPVariable_Wrap(rstd), kept);
     END_HANDLE_TH_ERRORS
