@@ -465,7 +465,8 @@ PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (c.given(4)) written(y);
     if (c.given(5)) written(sum);
     // x is h, but not where it holds y now.
-    PyObject* const kept = sum.defined() ? THPVariable_Wrap(sum) : o.data == r.data && r.n > 0 ? none() : Py_NewRef(c.args[0]);
+    if (!sum.defined() && x.requires_grad()) sum = x.detach();
+    PyObject* const kept = o.data == r.data && r.n > 0 && !c.given(2) ? none() : sum.defined() ? THPVariable_Wrap(sum) : Py_NewRef(c.args[0]);
     if (eight) return Py_BuildValue("(NNNN)", THPVariable_Wrap(y), THPVariable_Wrap(scale), THPVariable_Wrap(rstd), kept);
     return Py_BuildValue("(NNN)", THPVariable_Wrap(y), THPVariable_Wrap(rstd), kept);
     END_HANDLE_TH_ERRORS

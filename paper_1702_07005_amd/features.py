@@ -133,9 +133,9 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, sum_out=None, st
     """``h * rstd * weight`` over the last dimension, with ``h = x + residual`` and ``rstd = 1 / sqrt(mean(h ** 2) + eps)``;
     returns it with ``rstd`` (float32, one for each row) and ``h``, which ``rms_norm_grad`` takes.
 
-    The sum is rounded to ``x``'s type and normalised as it is kept; without a residual ``h`` is ``x``, or None where ``out``
-    takes ``x``'s place.  ``residual``: of ``x``'s type and shape; ``weight``: [dim], of ``x``'s type or float32, or None.
-    ``out`` and ``sum_out`` (for ``h``) may be ``x`` or ``residual``, but not the same."""
+    The sum is rounded to ``x``'s type and normalised as it is kept; without a residual ``h`` is ``x`` (detached if it requires
+    gradients), or None where ``out`` takes ``x``'s place.  ``residual``: of ``x``'s type and shape; ``weight``: [dim], of
+    ``x``'s type or float32, or None.  ``out`` and ``sum_out`` (for ``h``) may be ``x`` or ``residual``, but not the same."""
     if stream is None:
         d = _device()
         result = _features.rms_norm(d, _stream(d), x, weight, residual, eps, out, sum_out, None)

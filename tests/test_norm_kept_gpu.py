@@ -40,3 +40,20 @@ def test_kept_values_are_those_before_the_call(rows, dim):
 def test_kept_values_without_rows():
     x = torch.empty(0, 33, device=DEV)
     assert features.rms_norm(x, out=torch.empty_like(x))[2] is x
+
+
+# The calls are outside autograd: no result requires gradients, the caller's own x among them.
+@pytest.mark.parametrize("call", [features.rms_norm, features.rms_norm_8bit], ids=["rms_norm", "rms_norm_8bit"])
+def test_no_result_requires_gradients(call):
+    leaf = torch.randn(6, 64, device=DEV, requires_grad=True)
+    for x in (leaf, leaf * 2):
+        for res in (None, leaf):
+            results = call(x, leaf[0], res)
+            assert not any(t.requires_grad for t in results)
+            h = results[-1]
+            assert torch.equal(h, x.detach() if res is None else x.detach() + leaf.detach())
+            assert res is not None or (h.data_ptr() == x.data_ptr() and h._version == x._version)
+        with torch.no_grad():
+            assert not call(x)[-1].requires_grad
+    plain = leaf.detach()
+    assert call(plain)[-1] is plain
