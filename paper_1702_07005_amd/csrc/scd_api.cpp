@@ -581,7 +581,8 @@ int plan_epoch(const scd_solver* h, LaunchPlan* lp, uint32_t* n_groups) {
     lp->kind = skewed ? PLAN_MIXED : PLAN_GROUP;
     lp->long_len = (uint32_t)long_len;
     lp->tail = h->max_seg > (int64_t)G * slice_depth(G);
-    if (lp->kind == PLAN_GROUP) lp->drain = pipe_drain(h, window, groups);
+    // The mixed kernel: whether its batches come from the queue, which serves few workgroups.
+    if (lp->kind == PLAN_GROUP || groups <= cap_blocks) lp->drain = pipe_drain(h, window, groups);
     if (!skewed && pipe_ok) {
         groups = pipe_groups(h, window, groups);
         lp->kind = PLAN_PIPE;  // segments beyond the slices take its long path

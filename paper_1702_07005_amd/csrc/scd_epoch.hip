@@ -250,6 +250,18 @@ __global__ __launch_bounds__(256) void k_epoch_pipe(EpochArgs a) {
 constexpr int kQueueRing = 4;  // chunk bases held in LDS (chunk number mod 4)
 constexpr int kQueueLead = 4;  // steps between a claim and the first step of its chunk
 
+// The next of a.queue[0]'s positions (or batches), and the end of a workgroup's claims, which have returned: the last of
+// `workgroups` to get there resets both words for the next launch.
+__device__ __forceinline__ uint32_t queue_claim(const EpochArgs& a) {
+    return __hip_atomic_fetch_add(a.queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void queue_leave(const EpochArgs& a, uint32_t workgroups) {
+    if (__hip_atomic_fetch_add(a.queue + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == workgroups - 1) {
+        __hip_atomic_store(a.queue, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.queue + 1, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+}
+
 // Position of step `k` of this workgroup (>= n once the queue is exhausted).
 __device__ __forceinline__ uint32_t queue_pos(const uint32_t* ring, uint32_t k, uint32_t chunk) {
     return ring[(k / chunk) % kQueueRing] + k % chunk;
@@ -372,11 +384,7 @@ __global__ __launch_bounds__(256) void k_epoch_queue(EpochArgs a) {
     }
     if (lane == 0) {
         __builtin_amdgcn_s_waitcnt(0x0F70);  // every claim of this workgroup has been performed
-        const uint32_t done = __hip_atomic_fetch_add(a.queue + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (done == gridDim.x - 1) {  // the others have finished claiming: reset for the next launch
-            __hip_atomic_store(a.queue, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.queue + 1, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
+        queue_leave(a, gridDim.x);
     }
 }
 
@@ -386,7 +394,10 @@ __global__ __launch_bounds__(256) void k_epoch_queue(EpochArgs a) {
 // entries are processed by their group as in k_epoch_group; longer ones are handed to the
 // whole workgroup (LDS combine), one after the other, so that a long segment's gather-to-
 // scatter interval stays as short as a short segment's.  One barrier per batch (vote) plus
-// one per long segment.
+// one per long segment.  Few batches in flight (a.drain) are claimed in permutation order from the queue:
+// at a fixed stride workgroups that draw long segments fall behind (166,000 columns on 3,500 rows, 108 in
+// flight, gap ratio on one seed 2.73 at worst and above 2 in 5 runs of 300, in order 1.13 at worst of 100, at
+// 13.4 ms an epoch either way).
 // ----------------------------------------------------------------------------------------
 // `ng` (<= NG) groups of each workgroup take positions, so that gridDim.x * ng coordinates
 // are in flight at most.
@@ -395,11 +406,20 @@ __global__ __launch_bounds__(256) void k_epoch_mixed(EpochArgs a, uint32_t long_
     U* const uu = static_cast<U*>(a.u);
     constexpr int NG = 256 / G, NW = 4;
     __shared__ uint32_t longs[2][NG];
+    __shared__ uint32_t batch[2];
     __shared__ float part[2][NW];
     const int tid = threadIdx.x, lane = tid & (G - 1), grp = tid / G, wave = tid >> 6;
     const uint32_t n_batches = (a.perm.n + ng - 1) / ng;
     int lb = 0, pb = 0;
-    for (uint32_t b = blockIdx.x; b < n_batches; b += gridDim.x) {
+    uint32_t b = blockIdx.x;
+    if (a.drain) {
+        if (tid == 0) batch[1] = queue_claim(a);
+        __syncthreads();
+        b = batch[1];
+    }
+    while (b < n_batches) {
+        uint32_t next = b + gridDim.x;
+        if (a.drain && tid == 0) next = queue_claim(a);
         const uint32_t j = b * ng + grp;
         uint32_t my_long = 0xFFFFFFFFu;
         if ((uint32_t)grp < ng && j < a.perm.n) {
@@ -439,7 +459,9 @@ __global__ __launch_bounds__(256) void k_epoch_mixed(EpochArgs a, uint32_t long_
             }
         }
         if (lane == 0) longs[lb][grp] = my_long;
+        if (a.drain && tid == 0) batch[lb] = next;
         const int any_long = __syncthreads_or(my_long != 0xFFFFFFFFu);
+        if (a.drain) next = batch[lb];
         if (any_long) {
             for (int q = 0; q < NG; ++q) {
                 const uint32_t m = longs[lb][q];
@@ -463,13 +485,19 @@ __global__ __launch_bounds__(256) void k_epoch_mixed(EpochArgs a, uint32_t long_
             }
         }
         lb ^= 1;
+        b = next;
     }
+    if (a.drain && tid == 0) queue_leave(a, gridDim.x);
 }
 
 // ----------------------------------------------------------------------------------------
 // Epoch kernel, one workgroup of BS threads per coordinate (long segments): wave sums by
 // DPP, then the BS/64 wave sums through a double-buffered LDS array (one barrier per
-// coordinate).  ORDERED adds a device-scope fence and a barrier after the scatter so that
+// coordinate).  With a binding window (a.drain) the workgroups claim positions in permutation order from the
+// queue, one ahead: at a fixed stride they drift apart by hundreds of steps within an epoch, which departs from
+// the sequential algorithm more than the window does (rows of 370 entries on 166,000 columns, per-epoch gap ratio
+// on one seed 2.33 at worst and above 2 in 14 runs of 520, in order 1.41 at worst of 300, for 1.06 ms an epoch
+// instead of 0.96).  ORDERED adds a device-scope fence and a barrier after the scatter so that
 // with a single workgroup the next coordinate sees every update (sequential Alg. 1).
 // ----------------------------------------------------------------------------------------
 template <int FORM, int BS, int R, bool FRESH, bool ORDERED, typename U>
@@ -477,10 +505,18 @@ __global__ __launch_bounds__(BS) void k_epoch_block(EpochArgs a) {
     U* const uu = static_cast<U*>(a.u);
     constexpr int NW = BS / 64;
     __shared__ float part[2][NW];
+    __shared__ uint32_t pos[2];
     const int tid = threadIdx.x, wave = tid >> 6;
     int buf = 0;
     if (blockIdx.x >= a.n_groups) return;
-    for (uint32_t j = blockIdx.x; j < a.perm.n; j += a.n_groups) {
+    const bool queued = !ORDERED && a.drain;
+    uint32_t j = blockIdx.x;
+    if (queued) {
+        if (tid == 0) pos[1] = queue_claim(a);
+        __syncthreads();
+        j = pos[1];
+    }
+    while (j < a.perm.n) {
         if constexpr (!ORDERED) {
             // With a binding window every wave's atomics of the previous coordinate land before any
             // wave gathers this one, so a workgroup holds one coordinate between gather and scatter.
@@ -489,6 +525,8 @@ __global__ __launch_bounds__(BS) void k_epoch_block(EpochArgs a) {
                 __builtin_amdgcn_s_barrier();
             }
         }
+        uint32_t next = j + a.n_groups;
+        if (queued && tid == 0) next = queue_claim(a);
         const uint32_t m = perm_at(j, a.perm);
         const int64_t s0 = a.ptr[m], s1 = a.ptr[m + 1];
         const float m_old = a.model[m];
@@ -510,7 +548,9 @@ __global__ __launch_bounds__(BS) void k_epoch_block(EpochArgs a) {
             acc = fmaf(a.val[k], ld_u<FRESH>(uu + a.idx[k]), acc);
         acc = group_sum<64>(acc);
         if ((tid & 63) == 0) part[buf][wave] = acc;
+        if (queued && tid == 0) pos[buf] = next;
         __syncthreads();
+        if (queued) next = pos[buf];
         float g = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) g += part[buf][w];
@@ -529,7 +569,9 @@ __global__ __launch_bounds__(BS) void k_epoch_block(EpochArgs a) {
             __syncthreads();
         }
         buf ^= 1;
+        j = next;
     }
+    if (queued && tid == 0) queue_leave(a, a.n_groups);
 }
 
 // ----------------------------------------------------------------------------------------

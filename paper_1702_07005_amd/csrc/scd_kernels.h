@@ -45,10 +45,11 @@ struct EpochArgs {
                          // entry size (2 or 3), or kSpreadShift when u is the spread copy
     double* sink;        // pipelined kernel, fp64 shared vector: 256 slots per workgroup that
                          // inactive lanes add 0 to
-    uint32_t drain;      // wait for the group's own atomics before its next gathers (window binds)
+    uint32_t drain;      // wait for the group's own atomics before its next gathers (window binds); block and
+                         // mixed kernel: take positions from the queue
     uint32_t chunk;      // queued kernel: consecutive positions per claim (1..kQueueChunkMax)
-    uint32_t* queue;     // queued kernel: [0] next permutation position, [1] workgroups finished (both 0
-                         // between launches)
+    uint32_t* queue;     // queued, block and mixed kernel: [0] next permutation position (batch), [1] workgroups
+                         // finished (both 0 between launches)
 };
 
 constexpr uint32_t kQueueChunkMax = 64;
@@ -80,7 +81,8 @@ struct LaunchPlan {
     uint32_t long_len;  // PLAN_MIXED: segments longer than this go to the whole workgroup
     int tail;           // PLAN_GROUP: some segment is longer than the register slices
     int drain;          // PLAN_PIPE, PLAN_GROUP, PLAN_BLOCK: the window binds, so each group lets its scatter
-                        // land before it gathers again
+                        // land before it gathers again; PLAN_BLOCK, PLAN_MIXED: and positions (batches) come
+                        // from the queue
     int chunk;          // PLAN_QUEUE, PLAN_SPLIT: consecutive positions (units) per claim
     uint32_t part;      // PLAN_SPLIT: entries per part of a long segment (multiple of 64, <= kSplitMaxPart)
     int wide;           // shared vector stored as double
