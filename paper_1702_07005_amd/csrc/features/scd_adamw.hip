@@ -466,7 +466,8 @@ __global__ void __launch_bounds__(kStepThreads) k_adamw(StepArgs<EIGHT> a) {
         s.gt == SCD_F32 ? step(f16{}, float{}) : step(f16{}, f16{});
 }
 
-// Whether lines of all arrays of a tensor begin with its whole chunks.
+// Whether all arrays of a tensor have its whole chunks at the beginning of 64 bytes, the least that memory is written in: what
+// a chunk's stores fill need not be read first.  (kStepLine is coarser, 256 bytes of a state and 128 of an array of 16 bits.)
 template <bool EIGHT>
 bool whole_lines(const scd_adamw_span_t& t) {
     const int64_t at = -(int64_t)early<EIGHT>(t.m), state = EIGHT ? 1 : 4;

@@ -599,7 +599,7 @@ int64_t even_blocks(int64_t turns, int64_t most) { return ceil_div(turns, ceil_d
 // 5,120 121 and 129, 8,000 x 10,000 108 and 119, 8,192 x 12,288 116 and 128 (bf16); but of fourteen waves 4,096 x 14,336 89
 // and 78, and forward or in fp32 no width gains by it.  The backward pass's widest rows take 1,024 threads that load a row
 // when they come to it: 8,192 x 16,384 (bf16) 142 us, with 512 threads that load the next one ahead 169; 4,096 x 16,384
-// (fp32) 149 and 229.
+// (fp32) 149 and 229.  (These spill a few of their 128 registers, 6 to 16 with 16-bit elements and 27 in fp32.)
 template <typename T, bool GRAD, typename F>
 bool with_rms_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
@@ -619,17 +619,19 @@ bool with_rms_group(int64_t dim, F&& f) {
         if (waves == 11 || waves == 12) f(Int<V>{}, Int<2>{}, Int<768>{});
         if (waves <= 12 && waves != 8) return true;
     }
-    if (!GRAD || vecs <= 1024)
-        return with_group<T, GRAD>(dim, f);
-    else if (vecs <= 2048)
-        f(Int<V>{}, Int<2>{}, Int<1024>{});
-    else if constexpr (V == 4) {
-        if (vecs > 4096) return false;
-        f(Int<V>{}, Int<4>{}, Int<1024>{});
+    if constexpr (!GRAD) {
+        return with_group<T, false>(dim, f);
     } else {
-        return false;
+        if (vecs <= 1024)
+            with_usual_group<T, true>(dim, f);
+        else if (vecs <= 2048)
+            f(Int<V>{}, Int<2>{}, Int<1024>{});
+        else if (V == 4 && vecs <= 4096)
+            f(Int<V>{}, Int<V == 4 ? 4 : 2>{}, Int<1024>{});
+        else
+            return false;
+        return true;
     }
-    return true;
 }
 
 int check_rms(int32_t type, int32_t param_type, int64_t rows, int64_t dim) {

@@ -59,12 +59,10 @@ constexpr int kWideThreads = 1024;
 
 // ---------------------------------------------------------------------------------------- host
 
-// Calls f(Int<VEC>, Int<NV>, Int<LPR>) with the smallest group that holds a row of `dim` elements of T, or returns
-// false where none does.  A wave holds four vectors a lane, but in the backward pass, which keeps six values per element,
-// of 16-bit elements three; and the widest rows take 512 threads there, which may have 256 registers each, and 1,024 in
-// the forward pass.
+// Calls f(Int<VEC>, Int<NV>, Int<LPR>) with the smallest group that holds a row of `dim` elements of T, 1,024 vectors at most.
+// A wave holds four vectors a lane, but in the backward pass, which keeps six values per element, of 16-bit elements three.
 template <typename T, bool GRAD, typename F>
-bool with_group(int64_t dim, F&& f) {
+void with_usual_group(int64_t dim, F&& f) {
     constexpr int V = 16 / sizeof(T);
     const int64_t vecs = ceil_div(dim, V);
     if (dim < V)
@@ -87,8 +85,18 @@ bool with_group(int64_t dim, F&& f) {
         f(Int<V>{}, Int<GRAD && V == 8 ? 1 : 4>{}, Int<GRAD && V == 8 ? 256 : 64>{});
     else if (vecs <= 512)
         f(Int<V>{}, Int<2>{}, Int<256>{});
-    else if (vecs <= 1024)
+    else
         f(Int<V>{}, Int<2>{}, Int<512>{});
+}
+
+// The same for rows of any width, or returns false where no group holds one.  The widest rows take 512 threads in the backward
+// pass, which may have 256 registers each, and 1,024 in the forward pass.
+template <typename T, bool GRAD, typename F>
+bool with_group(int64_t dim, F&& f) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t vecs = ceil_div(dim, V);
+    if (vecs <= 1024)
+        with_usual_group<T, GRAD>(dim, f);
     else if (vecs <= 2048)
         f(Int<V>{}, Int<GRAD ? 4 : 2>{}, Int<GRAD ? 512 : 1024>{});
     else if constexpr (V == 4) {
