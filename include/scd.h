@@ -519,9 +519,11 @@ typedef struct {
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
  * Parameters move by m and v in 32 bits, before these are rounded; a NaN norm makes f NaN, an infinite one 0, as in
  * scd_clip_grads, so that with norm_dev the gradients need not be written clipped.
- * States of 8 bits: the scales are max(largest / 448, 2^-126) of the block's finite |m| and sqrt(v), others become NaN; m /
- * m_scale goes to one of its neighbours in 8 bits with probabilities that keep its mean, sqrt(v) / v_scale with those that keep the
- * mean of its square, but away from 0.  With fmix32 the finaliser of MurmurHash3, element i of the k-th tensor takes
+ * States of 8 bits: the scales are max(c largest, 2^-126) of the block's finite |m| and sqrt(v), c = 1 / 448 rounded to 32
+ * bits, others become NaN; m / m_scale goes to one of its neighbours in 8 bits with probabilities that keep its mean, sqrt(v) /
+ * v_scale with those that keep the mean of its square, but away from 0.  Every product, sum, quotient and root up to there is
+ * rounded to 32 bits; of |m| / m_scale below 2^-6 what lies below 2^-29 is cut off.  With fmix32 the finaliser of MurmurHash3,
+ * element i of the k-th tensor takes
  *   word = fmix32(low 32 bits of i xor (fmix32(fmix32(seed xor fmix32(low 32 bits of t)) + k) + high 32 bits of i)),
  * and goes away from 0 where (word mod 2^16 + 1/2) / 2^16 (m), (word / 2^16 + 1/2) / 2^16 (sqrt(v); word / 2^16 without
  * its fraction) is less than the probability of that.

@@ -217,9 +217,9 @@ __device__ __forceinline__ void chunk_32(const Common& c, const Step32& s, int64
 constexpr uint32_t kLargest = 0x7F7FFFFFu;  // bits of the largest finite number
 constexpr float kSmallRoot = 0x1p-96f;
 
-// The averages of a state in 8 bits.  Every product and sum rounds by itself, and scaled() and root() below as a division and
-// a square root do: a state that lies at the border between up and down goes the same way wherever these formulas are
-// computed in 32 bits.
+// The averages of a state in 8 bits.  Every product and sum rounds by itself, divide() and root() below as a division and a
+// square root do, and the scale is the product that the header states: a state that lies at the border between up and down
+// goes the same way wherever these formulas are computed in 32 bits.
 __device__ __forceinline__ void next_moments(const Common& c, float g, float m0, float r0, float& m, float& v) {
 #pragma clang fp contract(off)
     m = c.b1 * m0 + c.a1 * g;
@@ -397,7 +397,8 @@ __device__ __forceinline__ void blocks_8(const StepArgs<true>& a, const Step8& s
         most_r = block_most(most_r);
     }
     const float to_m = e4m3_scale(__uint_as_float(most_m)), to_r = e4m3_scale(__uint_as_float(most_r));
-    const float im = inverse(to_m), ir = inverse(to_r);
+    divide(m, to_m);
+    divide(r, to_r);
     const uint32_t key = murmur_fmix32(c.key + (uint32_t)s.place) + (uint32_t)((uint64_t)at >> 32);
 #pragma unroll
     for (int k = 0; k < V / 4; ++k) {
@@ -406,8 +407,7 @@ __device__ __forceinline__ void blocks_8(const StepArgs<true>& a, const Step8& s
         for (int l = 0; l < 4; ++l) {
             float& x = r[4 * k + l];
             word[l] = murmur_fmix32((uint32_t)(from + k * kApart + l) ^ key);
-            m[4 * k + l] = scaled(m[4 * k + l], to_m, im);
-            x = x == 0.0f ? 0.0f : fmaxf(scaled(x, to_r, ir), kLeast);
+            x = x == 0.0f ? 0.0f : fmaxf(x, kLeast);  // of r > 0 no quotient is 0: from 2^-75 to 2^64 they differ by 2^139
         }
         mw[k] = random_m4(m + 4 * k, word);
         rw[k] = random_r4(r + 4 * k, word) | lost[k];
