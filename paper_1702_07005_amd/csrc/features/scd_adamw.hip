@@ -14,7 +14,7 @@
 // becomes 0, where m over it would be without bound.  The random numbers are a hash of seed, step, tensor and element.
 //
 // Measured: 354 M weights (fp32, gradients and copies in bf16) 1,543 us with states of 32 bits, 6.4 TB/s of the 9.9 GB that
-// it cannot do without, and 909 us with 8, 6.3 TB/s of 5.7 GB, where the arithmetic (78 instructions an element) keeps the
+// it cannot do without, and 909 us with 8, 6.3 TB/s of 5.7 GB, where the arithmetic (77 instructions an element) keeps the
 // SIMDs busy for two thirds of that time; 11 tensors of 160,000 weights in all 3.8 and 4.7 us on the GPU.
 #include <algorithm>
 #include <cmath>
