@@ -453,7 +453,8 @@ int scd_clip_grads(const scd_span_t *spans, int64_t count, float max_norm, float
  * its scale, and the quotient, rounded to 32 bits, goes to the nearest value of 8, ties to even; scale = max(c largest |y|,
  * 2^-126) with c = 1 / 448 rounded to 32 bits.  group = 0: one scale for each row, scale_dev: float32[rows];  group = 32,
  * 64 or 128: one for each `group` columns (the last group may be shorter), scale_dev: float32[rows, ceil(dim / group)].  A
- * NaN gives NaN and does not count for the scale; an infinite y makes its scale infinite and itself NaN.  Otherwise group is 0 and scale_dev is unused.
+ * NaN gives NaN and does not count for the scale; an infinite y makes its scale infinite and itself NaN.  Otherwise group is
+ * 0 and scale_dev is unused.
  * y may be x or residual unless it has 8 bits, and sum may be x or residual, with the same stride; y is not sum.  Squares
  * are summed in 32 bits: rows whose mean square is beyond float32 give zeros. */
 int scd_rms_norm(const void *x_dev, int32_t type, int64_t x_stride, const void *residual_dev, int64_t residual_stride,

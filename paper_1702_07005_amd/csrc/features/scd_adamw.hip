@@ -348,8 +348,8 @@ __device__ __forceinline__ void blocks_8(const StepArgs<true>& a, const Step8& s
 #pragma unroll
         for (int k = 0; k < V; ++k) r[k] = root(r[k]);
     }
-    // The instruction takes a denormal number for 0, whose inverse makes NaN of an m of 0, and gives 0 for its inverse.  Without
-    // eps the sum is 0 or at least 2^-75, and r c.root stays below 2^91.
+    // The instruction takes a denormal number for 0, whose inverse makes NaN of an m of 0, and gives 0 instead of a denormal
+    // one.  Without eps the sum is 0 or at least 2^-75, and r c.root stays below 2^91.
     if (c.eps == 0.0f || (c.eps >= 0x1p-126f && c.eps <= 0x1p100f)) {
 #pragma unroll
         for (int k = 0; k < V; ++k) p[k] = p[k] * keep - c.rate * m[k] * __builtin_amdgcn_rcpf(r[k] * c.root + c.eps);
