@@ -246,6 +246,9 @@ __global__ __launch_bounds__(256) void k_epoch_pipe(EpochArgs a) {
 // when it loads the metadata of the chunk's first coordinate two steps ahead.  No wait or
 // barrier is added.  Each workgroup counts itself out in queue[1]; the last one resets both
 // words for the next launch.
+//
+// ONE: chunks of one position, without the divisions by a chunk's length (60,000 rows of 809 entries, 11 in flight: 20.6
+// ms an epoch instead of 21.2).
 // ----------------------------------------------------------------------------------------
 constexpr int kQueueRing = 4;  // chunk bases held in LDS (chunk number mod 4)
 constexpr int kQueueLead = 4;  // steps between a claim and the first step of its chunk
@@ -271,14 +274,14 @@ __device__ __forceinline__ uint32_t queue_pos(const uint32_t* ring, uint32_t k, 
 // and `nxt`'s metadata were loaded one step earlier.  Loads `nxt`'s segment into `ni/nv` and
 // the metadata of the coordinate two steps ahead into `nn`; returns that coordinate's position
 // (>= n when the queue is exhausted; `nn` then describes a valid stand-in coordinate).
-template <int FORM, int R, bool FRESH, typename U>
+template <int FORM, int R, bool FRESH, bool ONE, typename U>
 __device__ __forceinline__ uint32_t queue_step(const EpochArgs& a, const SharedBuf<U>& ub,
                                                const __amdgpu_buffer_rsrc_t& qr, int lane, uint32_t k,
                                                const CoordMeta& cur, const int (&ci)[R], const float (&cv)[R],
                                                const CoordMeta& nxt, int (&ni)[R], float (&nv)[R], CoordMeta& nn,
                                                uint32_t* ring, uint32_t& claim, float (*part)[4], int& buf) {
     constexpr int G = 256;
-    const uint32_t K = a.chunk;
+    const uint32_t K = ONE ? 1 : a.chunk;
     // vmcnt(0): this wave's atomics and its last claim have landed; the barrier extends that to the
     // atomics of all four waves before any of them gathers the next coordinate.
     __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -286,8 +289,10 @@ __device__ __forceinline__ uint32_t queue_step(const EpochArgs& a, const SharedB
     // The previous step claimed chunk (k - 1 + kQueueLead) / K if it began one.
     if (lane == 0 && k > 0 && (k - 1 + kQueueLead) % K == 0) ring[((k - 1 + kQueueLead) / K) % kQueueRing] = claim;
     const uint32_t n = a.perm.n;
-    const uint32_t p2 = queue_pos(ring, k + 2, K);  // its chunk was published before the previous barrier
-    const uint32_t m2 = p2 < n ? perm_at(p2, a.perm) : cur.m;
+    // Its chunk was published before the previous barrier.  The position is the workgroup's: its coordinate is computed by the
+    // scalar unit, behind the gathers (19.4 ms instead of the 20.6 above).
+    const uint32_t p2 = (uint32_t)__builtin_amdgcn_readfirstlane((int)queue_pos(ring, k + 2, K));
+    const auto ahead = [&] { return p2 < n ? perm_at(p2, a.perm) : cur.m; };
     const int qoff = lane == 0 && (k + kQueueLead) % K == 0 ? 0 : 4;
     const int64_t len = cur.s1 - cur.s0;
     if (len > (int64_t)G * R) {
@@ -298,7 +303,7 @@ __device__ __forceinline__ uint32_t queue_step(const EpochArgs& a, const SharedB
         a.model[cur.m] = m_new;
         if (coef != 0.0f) long_scatter<G>(a, ub, lane, cur.s0, cur.s1, coef);
         load_seg_raw<G, R>(a, nxt, lane, ni, nv);
-        nn = load_meta_of(a, m2);
+        nn = load_meta_of(a, ahead());
         claim = (uint32_t)__builtin_amdgcn_raw_ptr_buffer_atomic_add_i32((int)K, qr, qoff, 0, 0);
     } else {
         float gv[R];
@@ -306,7 +311,7 @@ __device__ __forceinline__ uint32_t queue_step(const EpochArgs& a, const SharedB
         for (int r = 0; r < R; ++r) gv[r] = buf_load<FRESH>(ub, (uint32_t)ci[r], (int64_t)(lane + r * G) < len);
         __builtin_amdgcn_sched_barrier(0);
         load_seg_raw<G, R>(a, nxt, lane, ni, nv);
-        nn = load_meta_of(a, m2);
+        nn = load_meta_of(a, ahead());
         claim = (uint32_t)__builtin_amdgcn_raw_ptr_buffer_atomic_add_i32((int)K, qr, qoff, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         float acc = 0.0f;
@@ -324,14 +329,14 @@ __device__ __forceinline__ uint32_t queue_step(const EpochArgs& a, const SharedB
     return p2;
 }
 
-template <int FORM, int R, bool FRESH, typename U>
+template <int FORM, int R, bool FRESH, bool ONE, typename U>
 __global__ __launch_bounds__(256) void k_epoch_queue(EpochArgs a) {
     constexpr int G = 256;
     __shared__ float part[2][G / 64];
     __shared__ uint32_t ring[kQueueRing];
     const int lane = threadIdx.x;
     const uint32_t n = a.perm.n;
-    const uint32_t K = a.chunk;
+    const uint32_t K = ONE ? 1 : a.chunk;
     // word 3 = 0x00020000: 32-bit data format, the gfx9-family raw-buffer setting.
     const __amdgpu_buffer_rsrc_t qr = __builtin_amdgcn_make_buffer_rsrc(a.queue, (short)0, 4, 0x00020000);
     // The chunks that cover steps [0, kQueueLead): the steps' own claims start with the next one.
@@ -371,10 +376,10 @@ __global__ __launch_bounds__(256) void k_epoch_queue(EpochArgs a) {
         CoordMeta cB = load_meta_of(a, pB < n ? perm_at(pB, a.perm) : cA.m);
         for (;;) {
             CoordMeta cA2, cB2;
-            const uint32_t pA2 = queue_step<FORM, R, FRESH>(a, ub, qr, lane, k++, cA, ciA, cvA, cB, ciB, cvB, cA2,
+            const uint32_t pA2 = queue_step<FORM, R, FRESH, ONE>(a, ub, qr, lane, k++, cA, ciA, cvA, cB, ciB, cvB, cA2,
                                                             ring, claim, part, buf);
             if (pB >= n) break;
-            const uint32_t pB2 = queue_step<FORM, R, FRESH>(a, ub, qr, lane, k++, cB, ciB, cvB, cA2, ciA, cvA, cB2,
+            const uint32_t pB2 = queue_step<FORM, R, FRESH, ONE>(a, ub, qr, lane, k++, cB, ciB, cvB, cA2, ciA, cvA, cB2,
                                                             ring, claim, part, buf);
             if (pA2 >= n) break;
             cA = cA2;
@@ -638,7 +643,10 @@ static hipError_t launch_pipe(const EpochArgs& a, int blocks, hipStream_t s) {
 
 template <int FORM, bool FRESH, typename U>
 static hipError_t launch_queue(const EpochArgs& a, int blocks, hipStream_t s) {
-    hipLaunchKernelGGL((k_epoch_queue<FORM, kQueueSlices, FRESH, U>), dim3(blocks), dim3(256), 0, s, a);
+    if (a.chunk == 1)
+        hipLaunchKernelGGL((k_epoch_queue<FORM, kQueueSlices, FRESH, true, U>), dim3(blocks), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_epoch_queue<FORM, kQueueSlices, FRESH, false, U>), dim3(blocks), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -658,7 +666,7 @@ static hipError_t launch_pipe_by_width(const EpochArgs& a, const LaunchPlan& lp,
         case 16: return launch_pipe<FORM, 16, FRESH, U>(a, lp.blocks, s);
         case 32: return launch_pipe<FORM, 32, FRESH, U>(a, lp.blocks, s);
         case 64: return launch_pipe<FORM, 64, FRESH, U>(a, lp.blocks, s);
-        case 256: return launch_pipe<FORM, 256, FRESH, U>(a, lp.blocks, s);
+        case 256: return lp.queued ? launch_queue<FORM, FRESH, U>(a, lp.blocks, s) : launch_pipe<FORM, 256, FRESH, U>(a, lp.blocks, s);
         default: return hipErrorInvalidValue;
     }
 }

@@ -83,6 +83,7 @@ struct LaunchPlan {
     int drain;          // PLAN_PIPE, PLAN_GROUP, PLAN_BLOCK: the window binds, so each group lets its scatter
                         // land before it gathers again; PLAN_BLOCK, PLAN_MIXED: and positions (batches) come
                         // from the queue
+    int queued;         // PLAN_PIPE with a workgroup per coordinate: positions come from the queue
     int chunk;          // PLAN_QUEUE, PLAN_SPLIT: consecutive positions (units) per claim
     uint32_t part;      // PLAN_SPLIT: entries per part of a long segment (multiple of 64, <= kSplitMaxPart)
     int wide;           // shared vector stored as double

@@ -1,5 +1,5 @@
-"""The plain kernels with few coordinates in flight take them in the order of the permutation, also where one workgroup draws
-all the long segments."""
+"""The plain kernels with few coordinates in flight, and the pipelined one with a workgroup for each of a given number, take them
+in the order of the permutation, also where one workgroup draws all the long segments."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -17,8 +17,8 @@ from paper_1702_07005_amd import scd, synth  # noqa: E402
 # Columns of ones on supports of their own, each twice: the one that comes first takes the whole of the labels there and leaves
 # the other nothing.  At a fixed stride one of four workgroups would draw all the first ones, which are long (explicit zeros),
 # and the others would long have reached the second ones, 50 turns later in the permutation.
-@pytest.mark.parametrize("kernel,lanes", [("block", 256), ("mixed", 64)])
-def test_plain_kernels_keep_the_order(kernel, lanes):
+@pytest.mark.parametrize("kernel,lanes", [("block", 256), ("mixed", 64), ("pipelined", 256)])
+def test_kernels_keep_the_order(kernel, lanes):
     turn = 256 // lanes                 # positions that a workgroup takes at a time
     pairs, apart, short, zeros, W = 200, 50, 300, 20_000, 4
     n = W * turn * (pairs + apart + 2)
@@ -39,7 +39,7 @@ def test_plain_kernels_keep_the_order(kernel, lanes):
     y = np.concatenate([np.ones(pairs * short), np.zeros(zeros)])
     dev = [torch.from_numpy(np.ascontiguousarray(t)).to("cuda") for t in (ptr.astype(np.int64), idx.astype(np.int32), val.astype(np.float32), y.astype(np.float32))]
     s = scd.Solver(L, n, *dev, 1e-9, "ridge_primal")
-    s.set_option("pipeline", 0)
+    s.set_option("pipeline", int(kernel == "pipelined"))
     s.set_option("group", lanes)
     s.set_option("window", W * turn)
     info = s.info()
